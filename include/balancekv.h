@@ -14,6 +14,8 @@
  *
  * and, on top of them, Alg. 1 as listed (value-norm buckets, numerator and denominator
  * instances): offline as bkv_balancekv_sets / bkv_attend_sets, token by token as bkv_stream_*.
+ * Beside them what a server does with such caches: bkv_attend_prefix (a batch that shares prefixes),
+ * bkv_attend_mass and bkv_evict (accumulated attention weight, and the eviction that goes by it).
  *
  * Conventions
  *  - Plain C, no exceptions.  Every tensor pointer is a DEVICE pointer owned by
@@ -203,6 +205,59 @@ size_t bkv_attend_kv_static_max_bytes(void);
 int bkv_attend_kv_static(const bkv_params* p, const void* K_c, const void* V_c, const float* w,
                          int64_t n_seq, int64_t count, int64_t stride_tokens, const void* Q, int32_t g,
                          int32_t nq, void* out, float* lse_out, void* hip_stream);
+
+/* ---- attention of a batch that shares prefixes -------------------------------------------------------
+ * n_seq sequences stand on n_pre prefixes, sequence s on prefix s mod n_pre (sessions x heads on the heads of one prompt;
+ * n_seq must be a multiple of n_pre); every sequence has tokens of its own behind its prefix.  Each query runs over both:
+ * out = (prefix sum + own sum) / (prefix denominator + own denominator), as if the prefix stood in front of every sequence's
+ * own cache, but a prefix is read once for all sequences on it.
+ * K_p, V_p      [n_pre, stride_p, d], w_p [n_pre, stride_p]: the first count_p places of every prefix are read.
+ * K_s, V_s      [n_seq, stride_s, d], w_s [n_seq, stride_s]: the first count_s places of every sequence are read.
+ *               A count may be 0 (its pointers are then not looked at).  A place whose weight is not above 0 holds no token,
+ *               whatever its rows hold (infinities and NaN too): sequences of different lengths share a count that way.
+ * Q, out, lse_out  as in bkv_attend_kv; out must not overlap Q.  A query that meets no token gives zeros and lse = -inf.
+ * Precision as in bkv_attend_kv.  The workspace may hold anything; calls that overlap in time must not share one.
+ * Limits: n_seq <= 65535, g * nq <= 262140, n_seq * g * nq < 2^31, counts <= 2^30 (else BKV_ESHAPE).                        */
+size_t bkv_attend_prefix_workspace_bytes(const bkv_params* p, int64_t n_pre, int64_t n_seq, int32_t g,
+                                         int32_t nq);   /* for any counts */
+int bkv_attend_prefix(const bkv_params* p, const void* K_p, const void* V_p, const float* w_p, int64_t n_pre,
+                      int64_t count_p, int64_t stride_p, const void* K_s, const void* V_s, const float* w_s,
+                      int64_t n_seq, int64_t count_s, int64_t stride_s, const void* Q, int32_t g, int32_t nq,
+                      void* out, float* lse_out, void* workspace, size_t ws_bytes, void* hip_stream);
+
+/* ---- attention that adds up how much weight every cached token gets ------------------------------------
+ * The estimator of bkv_attend_kv, and with P_ij = w_j e^{<k_j,q_i>/sqrt d} / sum_j' w_j' e^{<k_j',q_i>/sqrt d} the weight of
+ * token j in the answer to query i:
+ *   mass_out[s, j] = decay * mass_in[s, j] + sum of P_ij over the g * nq queries of sequence s,   j < count.
+ * K_c, V_c, w, Q, out, lse_out, count, stride_tokens, limits and precision as in bkv_attend_prefix (places without a token
+ * too: their P is 0).
+ * visible       query i (0 <= i < nq) of every head sees the first visible + i places (none where that is not above 0); from
+ *               `count` on all see everything.  The last nq tokens of a cache against it: count - nq + 1; a prompt against
+ *               itself: 1.
+ * mass_in       [n_seq, stride_tokens] fp32 or NULL (zeros); may be mass_out, no other overlap.  decay in [0, 1]; with 0 it is
+ *               not read.  mass_out [n_seq, stride_tokens]: places from `count` on are left as they are.  count == 0: untouched.
+ * The sums run in an order that depends on the shapes alone: the same call gives the same bits.                             */
+size_t bkv_attend_mass_workspace_bytes(const bkv_params* p, int64_t n_seq, int64_t count, int32_t g, int32_t nq);
+int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const float* w, int64_t n_seq,
+                    int64_t count, int64_t stride_tokens, const void* Q, int32_t g, int32_t nq, int64_t visible,
+                    float decay, const float* mass_in, void* out, float* lse_out, float* mass_out,
+                    void* workspace, size_t ws_bytes, void* hip_stream);
+
+/* ---- eviction by accumulated attention weight ----------------------------------------------------------
+ * Of the first `count` places of every sequence the first n_sink and the last n_recent stay, and the heaviest of the others,
+ * `keep` in all (ties go to the lowest place; -0 is 0, a NaN counts as -inf), in ascending order, with their own weights.
+ * A place whose weight w is not above 0 holds no token and never stays, in the windows neither.
+ * K_c, V_c      [n_seq, stride_tokens, d]; w, mass [n_seq, stride_tokens] fp32; idx_in [n_seq, stride_tokens] int32 or NULL.
+ * K_out, V_out  [n_seq, keep, d]; w_out, mass_out [n_seq, keep] fp32 or NULL; idx_out [n_seq, keep] int32 or NULL: idx_in of
+ *               every kept token, or its place.  count_out [n_seq] int32 or NULL: tokens kept; behind them rows, w and mass
+ *               are 0 and idx -1.
+ * BKV_EINVAL    keep > count, n_sink + n_recent > keep, or an output that overlaps an input or another output.
+ * Limits: n_seq <= 65535, count <= 2^30 (else BKV_ESHAPE).                                                                   */
+size_t bkv_evict_workspace_bytes(const bkv_params* p, int64_t n_seq, int64_t count);
+int bkv_evict(const bkv_params* p, const void* K_c, const void* V_c, const float* w, const float* mass,
+              const int32_t* idx_in, int64_t n_seq, int64_t count, int64_t stride_tokens, int64_t keep,
+              int64_t n_sink, int64_t n_recent, void* K_out, void* V_out, float* w_out, float* mass_out,
+              int32_t* idx_out, int32_t* count_out, void* workspace, size_t ws_bytes, void* hip_stream);
 
 /* ---- Alg. 1 as listed: value-norm buckets, MR-Numerator_i per bucket, MR-Denominator ---------------
  * Offline form on K, V [n_seq, n, d] (any n >= 0): every instance is brought to the state Alg. 3

@@ -53,6 +53,13 @@ _SIGNATURES = {
     "bkv_attend_kv": (C.c_int, [_PP, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _i32, _i32, _vp, _vp, _vp, _sz, _vp]),
     "bkv_attend_kv_static_max_bytes": (_sz, []),
     "bkv_attend_kv_static": (C.c_int, [_PP, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _i32, _i32, _vp, _vp, _vp]),
+    "bkv_attend_prefix_workspace_bytes": (_sz, [_PP, _i64, _i64, _i32, _i32]),
+    "bkv_attend_prefix": (C.c_int, [_PP, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _i32, _i32, _vp, _vp,
+                                    _vp, _sz, _vp]),
+    "bkv_attend_mass_workspace_bytes": (_sz, [_PP, _i64, _i64, _i32, _i32]),
+    "bkv_attend_mass": (C.c_int, [_PP, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _i32, _i32, _i64, C.c_float, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "bkv_evict_workspace_bytes": (_sz, [_PP, _i64, _i64]),
+    "bkv_evict": (C.c_int, [_PP, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "bkv_sets_capacity": (_i64, [_PP, _i64, _i32]),
     "bkv_balancekv_sets_workspace_bytes": (_sz, [_PP, _i64, _i64, _i64]),
     "bkv_balancekv_sets": (C.c_int, [_PP, _i32, _vp, _vp, _i64, _i64, _i64, C.c_float, C.c_float, _vp, _vp, _vp, _vp, _i64,
@@ -280,6 +287,128 @@ def attend_kv_static(p, K_c, V_c, w, Q, out, lse=None, *, count=None):
                                     _ptr(lse, torch.float32, "lse"), _stream())
     _check(rc, "bkv_attend_kv_static")
     return out, lse
+
+
+# ------------------------------------------------------------------------------------------ serving: prefix, mass, eviction
+def _here(first, *others):
+    """All tensors on the current device (the stream is this device's), like `first`."""
+    dev = first.device
+    if dev.type != "cuda":
+        raise ValueError("tensors must live on the GPU")
+    if dev.index != torch.cuda.current_device():
+        raise ValueError("tensors live on %s, the current device is cuda:%d" % (dev, torch.cuda.current_device()))
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError("tensors live on %s and on %s" % (dev, t.device))
+
+
+def _shaped(t, shape, what):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s, got %s" % (what, list(shape), list(t.shape)))
+
+
+def _rows(K, V, w, p, what):
+    """(sequences, places) of a weighted cache after looking at its shapes."""
+    if K.dim() != 3 or K.shape[2] != p.d:
+        raise ValueError("K%s must be [sequences, places, %d], got %s" % (what, p.d, list(K.shape)))
+    _shaped(V, K.shape, "V" + what)
+    _shaped(w, K.shape[:2], "w" + what)
+    return K.shape[0], K.shape[1]
+
+
+def attend_prefix_workspace_bytes(p, n_pre, n_seq, g, nq) -> int:
+    return int(lib().bkv_attend_prefix_workspace_bytes(C.byref(p), n_pre, n_seq, g, nq))
+
+
+def attend_prefix(p, prefix, own, Q, *, count_prefix=None, count_own=None, workspace=None, out=None, lse=True):
+    """bkv_attend_prefix: prefix = (K, V, w) of n_pre prefixes, own = (K, V, w) of n_seq sequences, sequence s on prefix
+    s mod n_pre; Q [n_seq, g, nq, d].  Returns (out, lse or None)."""
+    dt = _torch_dtype(p)
+    (Kp, Vp, wp), (Ks, Vs, ws) = prefix, own
+    n_pre, stride_p = _rows(Kp, Vp, wp, p, " of the prefix")
+    n_seq, stride_s = _rows(Ks, Vs, ws, p, " of the sequences")
+    _, g, nq, d = Q.shape
+    _shaped(Q, (n_seq, g, nq, p.d), "Q")
+    _here(Q, Kp, Vp, wp, Ks, Vs, ws, workspace, out)
+    if out is None:
+        out = Q.new_empty((n_seq, g, nq, d), dtype=dt)
+    _shaped(out, Q.shape, "out")
+    lse_t = Q.new_empty((n_seq, g, nq), dtype=torch.float32) if lse else None
+    if workspace is None:
+        workspace = torch.empty(attend_prefix_workspace_bytes(p, n_pre, n_seq, g, nq), device=Q.device, dtype=torch.uint8)
+    f32 = torch.float32
+    rc = lib().bkv_attend_prefix(C.byref(p), _ptr(Kp, dt, "K of the prefix"), _ptr(Vp, dt, "V of the prefix"), _ptr(wp, f32, "w of the prefix"),
+                                 n_pre, stride_p if count_prefix is None else count_prefix, stride_p, _ptr(Ks, dt, "K of the sequences"),
+                                 _ptr(Vs, dt, "V of the sequences"), _ptr(ws, f32, "w of the sequences"), n_seq,
+                                 stride_s if count_own is None else count_own, stride_s, _ptr(Q, dt, "Q"), g, nq, _ptr(out, dt, "out"),
+                                 _ptr(lse_t), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream())
+    _check(rc, "bkv_attend_prefix")
+    return out, lse_t
+
+
+def attend_mass_workspace_bytes(p, n_seq, count, g, nq) -> int:
+    return int(lib().bkv_attend_mass_workspace_bytes(C.byref(p), n_seq, count, g, nq))
+
+
+def attend_mass(p, K_c, V_c, w, Q, mass=None, *, count=None, visible=None, decay=1.0, mass_out=None, workspace=None, out=None, lse=True):
+    """bkv_attend_mass: attend_kv, and the tokens' accumulated attention weight.  K_c, V_c [n_seq, stride, d]; w, mass
+    [n_seq, stride] (mass None: zeros); Q [n_seq, g, nq, d]; query i sees the first visible + i places (None: all).  mass_out
+    may be mass.  Returns (out, lse or None, mass_out); a new mass_out is 0 from `count` on."""
+    dt = _torch_dtype(p)
+    n_seq, stride = _rows(K_c, V_c, w, p, "_c")
+    _, g, nq, d = Q.shape
+    _shaped(Q, (n_seq, g, nq, p.d), "Q")
+    _shaped(mass, (n_seq, stride), "mass")
+    _shaped(mass_out, (n_seq, stride), "mass_out")
+    _here(Q, K_c, V_c, w, mass, mass_out, workspace, out)
+    if count is None:
+        count = stride
+    if visible is None:
+        visible = count
+    if out is None:
+        out = Q.new_empty((n_seq, g, nq, d), dtype=dt)
+    _shaped(out, Q.shape, "out")
+    lse_t = Q.new_empty((n_seq, g, nq), dtype=torch.float32) if lse else None
+    if mass_out is None:
+        mass_out = w.new_empty((n_seq, stride)) if count == stride else w.new_zeros((n_seq, stride))
+    if workspace is None:
+        workspace = torch.empty(attend_mass_workspace_bytes(p, n_seq, count, g, nq), device=Q.device, dtype=torch.uint8)
+    f32 = torch.float32
+    rc = lib().bkv_attend_mass(C.byref(p), _ptr(K_c, dt, "K_c"), _ptr(V_c, dt, "V_c"), _ptr(w, f32, "w"), n_seq, count, stride, _ptr(Q, dt, "Q"),
+                               g, nq, max(min(visible, 1 << 40), -(1 << 40)), float(decay), _ptr(mass, f32, "mass"), _ptr(out, dt, "out"),
+                               _ptr(lse_t), _ptr(mass_out, f32, "mass_out"), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                               _stream())
+    _check(rc, "bkv_attend_mass")
+    return out, lse_t, mass_out
+
+
+def evict_workspace_bytes(p, n_seq, count) -> int:
+    return int(lib().bkv_evict_workspace_bytes(C.byref(p), n_seq, count))
+
+
+def evict(p, K_c, V_c, w, mass, keep, *, n_sink=0, n_recent=0, count=None, idx=None, workspace=None):
+    """bkv_evict: the heaviest `keep` tokens of every sequence by mass [n_seq, stride], the first n_sink and the last n_recent
+    among them.  Returns dict(K, V, w, mass, idx [n_seq, keep], count [n_seq])."""
+    dt = _torch_dtype(p)
+    n_seq, stride = _rows(K_c, V_c, w, p, "_c")
+    _shaped(mass, (n_seq, stride), "mass")
+    _shaped(idx, (n_seq, stride), "idx")
+    _here(K_c, V_c, w, mass, idx, workspace)
+    if count is None:
+        count = stride
+    if not 0 <= keep <= count <= stride:
+        raise ValueError("keep %d of %d places, %d stored" % (keep, count, stride))
+    new, f32 = K_c.new_empty, torch.float32
+    res = dict(K=new((n_seq, keep, p.d), dtype=dt), V=new((n_seq, keep, p.d), dtype=dt), w=new((n_seq, keep), dtype=f32),
+               mass=new((n_seq, keep), dtype=f32), idx=new((n_seq, keep), dtype=torch.int32), count=new((n_seq,), dtype=torch.int32))
+    if workspace is None:
+        workspace = torch.empty(evict_workspace_bytes(p, n_seq, count), device=K_c.device, dtype=torch.uint8)
+    rc = lib().bkv_evict(C.byref(p), _ptr(K_c, dt, "K_c"), _ptr(V_c, dt, "V_c"), _ptr(w, f32, "w"), _ptr(mass, f32, "mass"),
+                         _ptr(idx, torch.int32, "idx"), n_seq, count, stride, keep, n_sink, n_recent, _ptr(res["K"]), _ptr(res["V"]),
+                         _ptr(res["w"]), _ptr(res["mass"]), _ptr(res["idx"]), _ptr(res["count"]), _ptr(workspace),
+                         workspace.numel() * workspace.element_size(), _stream())
+    _check(rc, "bkv_evict")
+    return res
 
 
 # ------------------------------------------------------------------------------------------ Alg. 1: buckets, two instances

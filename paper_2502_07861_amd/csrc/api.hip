@@ -407,6 +407,181 @@ int bkv_attend_kv_static(const bkv_params* p, const void* K_c, const void* V_c, 
                           bkv::kAttendStaticScratchBytes, true, hip_stream);
 }
 
+// ------------------------------------------------------------------------------------------ serving: prefix, mass, eviction
+}  // extern "C"
+
+static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && na && nb && x < y + nb && y < x + na;
+}
+
+// The two jobs of a batch on shared prefixes; the fan-out is n_seq / n_pre.
+static void prefix_jobs(bkv::TileJob& pre, bkv::TileJob& own, int64_t n_pre, int64_t n_seq, int n_q) {
+    memset(&pre, 0, sizeof(pre));
+    memset(&own, 0, sizeof(own));
+    pre.n_streams = (int32_t)n_pre; pre.rows = (int32_t)(n_seq / n_pre * n_q); pre.inner = n_q;
+    pre.q_stream = n_q; pre.q_outer = n_pre * n_q; pre.q_inner = 1;
+    own.n_streams = (int32_t)n_seq; own.rows = n_q; own.inner = n_q;
+    own.q_stream = n_q; own.q_outer = 0; own.q_inner = 1;
+}
+
+static void tile_common(bkv::TileArgs& a, const bkv_params* p, const void* Q, void* out, float* lse_out, int64_t n_rows) {
+    memset(&a, 0, sizeof(a));
+    a.Q = (const char*)Q; a.out = (char*)out; a.lse = lse_out; a.n_rows = n_rows;
+    a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)p->d));
+    a.inv_scale = (float)(sqrt((double)p->d) / 1.4426950408889634);
+}
+
+// Shapes that every attention of this section takes: what attend_kv takes, with at most 2^31 - 1 queries in all.
+static int check_queries(const bkv_params* p, int64_t n_seq, int32_t g, int32_t nq) {
+    const int rc = check_params(p);
+    if (rc) return rc;
+    if (n_seq < 0 || g <= 0 || nq <= 0) return BKV_EINVAL;
+    if (n_seq > 65535 || (int64_t)g * nq > 4 * 65535 || n_seq * g * nq > 0x7fffffffll) return BKV_ESHAPE;
+    return BKV_OK;
+}
+
+static int fill_empty(const bkv_params* p, int64_t n_rows, void* out, float* lse_out, hipStream_t st) {
+    hipError_t e = bkv::launch_fill_u32(out, 0u, n_rows * (int64_t)row_bytes(p) / 4, st);
+    if (e == hipSuccess && lse_out) e = bkv::launch_fill_u32(lse_out, 0xff800000u, n_rows, st);
+    return e == hipSuccess ? BKV_OK : hip_fail(e);
+}
+
+extern "C" {
+
+size_t bkv_attend_prefix_workspace_bytes(const bkv_params* p, int64_t n_pre, int64_t n_seq, int32_t g, int32_t nq) {
+    if (check_queries(p, n_seq, g, nq) || n_pre <= 0 || n_seq % n_pre) return 0;
+    const int splits = bkv::tile_most_splits(n_pre, n_seq / n_pre * g * nq) + bkv::tile_most_splits(n_seq, (int64_t)g * nq);
+    return align_up(bkv::tile_part_bytes(p->d, n_seq * g * nq, splits), 256);
+}
+
+int bkv_attend_prefix(const bkv_params* p, const void* K_p, const void* V_p, const float* w_p, int64_t n_pre, int64_t count_p,
+                      int64_t stride_p, const void* K_s, const void* V_s, const float* w_s, int64_t n_seq, int64_t count_s,
+                      int64_t stride_s, const void* Q, int32_t g, int32_t nq, void* out, float* lse_out, void* workspace,
+                      size_t ws_bytes, void* hip_stream) {
+    const int rc = check_queries(p, n_seq, g, nq);
+    if (rc) return rc;
+    if (n_pre <= 0 || n_seq % n_pre || count_p < 0 || stride_p < count_p || count_s < 0 || stride_s < count_s) return BKV_EINVAL;
+    if (n_seq == 0) return BKV_OK;
+    if (count_p > (1 << 30) || count_s > (1 << 30)) return BKV_ESHAPE;
+    if (!Q || !out || !aligned16(Q) || !aligned16(out)) return BKV_EINVAL;
+    const int n_q = g * nq;
+    const size_t q_bytes = (size_t)n_seq * n_q * row_bytes(p);
+    if (overlap(Q, q_bytes, out, q_bytes)) return BKV_EINVAL;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (count_p == 0 && count_s == 0) return fill_empty(p, n_seq * n_q, out, lse_out, st);
+    if (count_p > 0 && (!K_p || !V_p || !w_p || !aligned16(K_p) || !aligned16(V_p))) return BKV_EINVAL;
+    if (count_s > 0 && (!K_s || !V_s || !w_s || !aligned16(K_s) || !aligned16(V_s))) return BKV_EINVAL;
+    if (!workspace || ws_bytes < bkv_attend_prefix_workspace_bytes(p, n_pre, n_seq, g, nq) || !aligned16(workspace)) return BKV_EWORKSPACE;
+    bkv::TileArgs a;
+    tile_common(a, p, Q, out, lse_out, n_seq * n_q);
+    bkv::TileJob pre, own;
+    prefix_jobs(pre, own, n_pre, n_seq, n_q);
+    pre.K = (const char*)K_p; pre.V = (const char*)V_p; pre.w = w_p; pre.stride = stride_p; pre.count = (int32_t)count_p;
+    own.K = (const char*)K_s; own.V = (const char*)V_s; own.w = w_s; own.stride = stride_s; own.count = (int32_t)count_s;
+    int jobs = 0;
+    if (count_p > 0) a.job[jobs++] = pre;
+    if (count_s > 0) a.job[jobs++] = own;
+    for (int k = 0; k < jobs; ++k) bkv::tile_plan(a.job[k]);
+    const hipError_t e = bkv::launch_tiles(p->dtype, p->d, a, jobs, (float*)workspace, st);
+    return e == hipSuccess ? BKV_OK : hip_fail(e);
+}
+
+size_t bkv_attend_mass_workspace_bytes(const bkv_params* p, int64_t n_seq, int64_t count, int32_t g, int32_t nq) {
+    if (check_queries(p, n_seq, g, nq) || count < 0) return 0;
+    const int64_t n_q = (int64_t)g * nq;
+    const int splits = bkv::tile_most_splits(n_seq, n_q);
+    return align_up((size_t)n_seq * n_q * 8, 256) + (splits > 1 ? align_up(bkv::tile_part_bytes(p->d, n_seq * n_q, splits), 256) : 0) +
+           bkv::mass_part_bytes();
+}
+
+int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const float* w, int64_t n_seq, int64_t count,
+                    int64_t stride_tokens, const void* Q, int32_t g, int32_t nq, int64_t visible, float decay, const float* mass_in,
+                    void* out, float* lse_out, float* mass_out, void* workspace, size_t ws_bytes, void* hip_stream) {
+    const int rc = check_queries(p, n_seq, g, nq);
+    if (rc) return rc;
+    if (count < 0 || stride_tokens < count || !(decay >= 0.f && decay <= 1.f)) return BKV_EINVAL;
+    if (n_seq == 0) return BKV_OK;
+    if (count > (1 << 30)) return BKV_ESHAPE;
+    if (!Q || !out || !aligned16(Q) || !aligned16(out)) return BKV_EINVAL;
+    const int n_q = g * nq;
+    const size_t q_bytes = (size_t)n_seq * n_q * row_bytes(p);
+    if (overlap(Q, q_bytes, out, q_bytes)) return BKV_EINVAL;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (count == 0) return fill_empty(p, n_seq * n_q, out, lse_out, st);
+    if (!K_c || !V_c || !w || !mass_out || !aligned16(K_c) || !aligned16(V_c)) return BKV_EINVAL;
+    const size_t m_bytes = ((size_t)(n_seq - 1) * stride_tokens + count) * 4;
+    if (mass_in != mass_out && overlap(mass_in, m_bytes, mass_out, m_bytes)) return BKV_EINVAL;
+    if (overlap(w, m_bytes, mass_out, m_bytes)) return BKV_EINVAL;
+    if (!workspace || ws_bytes < bkv_attend_mass_workspace_bytes(p, n_seq, count, g, nq) || !aligned16(workspace)) return BKV_EWORKSPACE;
+    // rows of a cache in the order of their positions, its query heads next to each other
+    bkv::TileArgs a;
+    tile_common(a, p, Q, out, lse_out, n_seq * n_q);
+    bkv::TileJob& j = a.job[0];
+    j.K = (const char*)K_c; j.V = (const char*)V_c; j.w = w; j.stride = stride_tokens; j.count = (int32_t)count;
+    j.n_streams = (int32_t)n_seq; j.rows = n_q; j.inner = g; j.q_stream = n_q; j.q_outer = 1; j.q_inner = nq;
+    a.causal = visible < count;
+    a.visible = visible < -(int64_t)nq ? -(int64_t)nq : visible;
+    char* ws = (char*)workspace;
+    a.stats = (float*)ws;
+    ws += align_up((size_t)n_seq * n_q * 8, 256);
+    bkv::tile_plan(j);
+    hipError_t e = bkv::launch_tiles(p->dtype, p->d, a, 1, (float*)ws, st);
+    if (e != hipSuccess) return hip_fail(e);
+    const int splits = bkv::tile_most_splits(n_seq, n_q);
+    if (splits > 1) ws += align_up(bkv::tile_part_bytes(p->d, n_seq * n_q, splits), 256);
+    bkv::MassArgs b;
+    memset(&b, 0, sizeof(b));
+    b.K = (const char*)K_c; b.w = w; b.Q = (const char*)Q; b.stats = a.stats; b.mass = decay > 0.f ? mass_in : nullptr; b.mass_out = mass_out;
+    b.stride = stride_tokens; b.n_seq = n_seq; b.q_stream = j.q_stream; b.q_outer = j.q_outer; b.q_inner = j.q_inner;
+    b.visible = a.visible; b.count = (int32_t)count; b.rows = n_q; b.inner = g; b.causal = a.causal;
+    b.scale_log2 = a.scale_log2; b.inv_scale = a.inv_scale; b.decay = decay; b.part = (float*)ws;
+    e = bkv::launch_mass(p->dtype, p->d, b, st);
+    return e == hipSuccess ? BKV_OK : hip_fail(e);
+}
+
+size_t bkv_evict_workspace_bytes(const bkv_params* p, int64_t n_seq, int64_t count) {
+    if (check_params(p) || n_seq < 0 || n_seq > 65535 || count < 0 || count > (1 << 30)) return 0;
+    return align_up(bkv::evict_workspace_bytes(n_seq, count), 256) + 256;
+}
+
+int bkv_evict(const bkv_params* p, const void* K_c, const void* V_c, const float* w, const float* mass, const int32_t* idx_in,
+              int64_t n_seq, int64_t count, int64_t stride_tokens, int64_t keep, int64_t n_sink, int64_t n_recent, void* K_out,
+              void* V_out, float* w_out, float* mass_out, int32_t* idx_out, int32_t* count_out, void* workspace, size_t ws_bytes,
+              void* hip_stream) {
+    const int rc = check_params(p);
+    if (rc) return rc;
+    if (n_seq < 0 || count < 0 || stride_tokens < count || keep < 0 || keep > count || n_sink < 0 || n_recent < 0) return BKV_EINVAL;
+    if (n_sink > keep || n_recent > keep - n_sink) return BKV_EINVAL;
+    if (n_seq == 0) return BKV_OK;
+    if (n_seq > 65535 || count > (1 << 30)) return BKV_ESHAPE;
+    hipStream_t st = (hipStream_t)hip_stream;
+    hipError_t e;
+    if (keep == 0) {
+        if (count_out && (e = bkv::launch_fill_u32(count_out, 0u, n_seq, st)) != hipSuccess) return hip_fail(e);
+        return BKV_OK;
+    }
+    if (!K_c || !V_c || !w || !mass || !K_out || !V_out) return BKV_EINVAL;
+    if (!aligned16(K_c) || !aligned16(V_c) || !aligned16(K_out) || !aligned16(V_out)) return BKV_EINVAL;
+    // rows move in any order: no output may lie on anything that is read or written beside it
+    const size_t in_tok = (size_t)(n_seq - 1) * stride_tokens + count, out_tok = (size_t)n_seq * keep, rb = row_bytes(p);
+    const struct { const void* at; size_t n; } in[5] = {{K_c, in_tok * rb}, {V_c, in_tok * rb}, {w, in_tok * 4}, {mass, in_tok * 4}, {idx_in, in_tok * 4}},
+        res[6] = {{K_out, out_tok * rb}, {V_out, out_tok * rb}, {w_out, out_tok * 4}, {mass_out, out_tok * 4}, {idx_out, out_tok * 4}, {count_out, (size_t)n_seq * 4}};
+    for (int i = 0; i < 6; ++i) {
+        for (int k = 0; k < 5; ++k) if (overlap(res[i].at, res[i].n, in[k].at, in[k].n)) return BKV_EINVAL;
+        for (int k = 0; k < i; ++k) if (overlap(res[i].at, res[i].n, res[k].at, res[k].n)) return BKV_EINVAL;
+    }
+    if (!workspace || ws_bytes < bkv_evict_workspace_bytes(p, n_seq, count) || !aligned16(workspace)) return BKV_EWORKSPACE;
+    bkv::EvictArgs a;
+    memset(&a, 0, sizeof(a));
+    a.K = (const char*)K_c; a.V = (const char*)V_c; a.w = w; a.mass = mass; a.idx = idx_in;
+    a.K_out = (char*)K_out; a.V_out = (char*)V_out; a.w_out = w_out; a.mass_out = mass_out; a.idx_out = idx_out; a.count_out = count_out;
+    a.n_seq = n_seq; a.stride = stride_tokens; a.count = (int32_t)count; a.keep = (int32_t)keep; a.n_sink = (int32_t)n_sink;
+    a.n_recent = (int32_t)n_recent; a.row_bytes = (int32_t)rb;
+    e = bkv::launch_evict(a, workspace, st);
+    return e == hipSuccess ? BKV_OK : hip_fail(e);
+}
+
 // ------------------------------------------------------------------------------------------ Alg. 1: buckets, two instances
 int64_t bkv_sets_capacity(const bkv_params* p, int64_t n, int32_t max_buckets) {
     if (check_params(p) || n < 0 || max_buckets < 1) return 0;

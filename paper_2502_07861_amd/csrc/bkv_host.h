@@ -222,4 +222,74 @@ constexpr size_t kAttendPartialBytes = (size_t)1 << 40;                         
 size_t attend_scratch_bytes(int dtype, int d, int64_t n_seq, int64_t count, int n_q, size_t max_bytes);
 hipError_t attend_static_scratch(void** ptr);
 
+// Many queries against caches (tiles.hip).  A job is n_streams caches with `rows` queries each; row r of cache s is row
+// s q_stream + (r / inner) q_outer + (r % inner) q_inner of Q and of the outputs.
+struct TileJob {
+    const char* K;            // [n_streams, stride, d]
+    const char* V;
+    const float* w;           // [n_streams, stride]
+    int64_t stride;
+    int64_t q_stream, q_outer, q_inner;
+    int32_t count, n_streams, rows, inner;
+    // set by tile_plan: query tiles of 32 that a workgroup takes, workgroups per cache and split, splits, tiles of keys in one
+    int32_t qw, n_qt, splits, tiles_per_split;
+    float* part;              // set by the launcher: [splits, n_rows, d + pad], null: results are written
+};
+struct TileArgs {
+    TileJob job[2];
+    const char* Q;
+    char* out;
+    float* lse;               // or null
+    float* stats;             // [n_rows, 2] or null: reference exponent and 1 / denominator of a query
+    int64_t n_rows;           // queries in all
+    int64_t visible;          // causal: a query of outer index i sees the first visible + i tokens
+    int32_t causal;
+    float scale_log2, inv_scale;     // log2(e) / sqrt(d), and its inverse
+    uint32_t first;           // set by the launcher: workgroups of job 0
+};
+int tile_most_splits(int64_t n_streams, int64_t rows);
+void tile_plan(TileJob& j);
+size_t tile_part_bytes(int d, int64_t n_rows, int splits);
+// part: room for the partial rows of all splits of all jobs, if they are more than one
+hipError_t launch_tiles(int dtype, int d, TileArgs& a, int n_jobs, float* part, hipStream_t st);
+
+// mass_out[j] = decay mass[j] + sum over the queries of a cache of their attention weight on token j (mass.hip), from the queries'
+// statistics: TileArgs::stats of the pass in front.
+struct MassArgs {
+    const char* K;            // [n_seq, stride, d]
+    const float* w;           // [n_seq, stride]
+    const char* Q;
+    const float* stats;
+    const float* mass;        // [n_seq, stride] or null (decay is then 0)
+    float* mass_out;
+    int64_t stride, n_seq, q_stream, q_outer, q_inner, visible;
+    int32_t count, rows, inner, causal;
+    float scale_log2, inv_scale, decay;
+    // set by mass_plan
+    int32_t splits, rows_per_split, n_kb;
+    float* part;              // [splits, n_seq, count] where there are several
+};
+size_t mass_part_bytes();                             // what MassArgs::part takes at most, for any shape
+hipError_t launch_mass(int dtype, int d, MassArgs& a, hipStream_t st);
+
+// The heaviest tokens of a cache (evict.hip).
+struct EvictArgs {
+    const char* K;            // [n_seq, stride, d]
+    const char* V;
+    const float* w;           // [n_seq, stride], mass likewise
+    const float* mass;
+    const int32_t* idx;       // [n_seq, stride] or null
+    char* K_out;              // [n_seq, keep, d]
+    char* V_out;
+    float* w_out;             // [n_seq, keep] or null, mass_out and idx_out likewise
+    float* mass_out;
+    int32_t* idx_out;
+    int32_t* count_out;       // [n_seq] or null
+    int64_t n_seq, stride;
+    int32_t count, keep, n_sink, n_recent, row_bytes;
+    int32_t* pick;            // workspace [n_seq, keep]: place of every kept token, ascending, -1 behind the last one
+};
+size_t evict_workspace_bytes(int64_t n_seq, int64_t count);
+hipError_t launch_evict(EvictArgs& a, void* workspace, hipStream_t st);
+
 }  // namespace bkv
