@@ -287,7 +287,11 @@ struct EvictArgs {
     int32_t* count_out;       // [n_seq] or null
     int64_t n_seq, stride;
     int32_t count, keep, n_sink, n_recent, row_bytes;
-    int32_t* pick;            // workspace [n_seq, keep]: place of every kept token, ascending, -1 behind the last one
+    // workspace: [n_seq, keep] place of every kept token, ascending, -1 behind the last one; long sequences: counts of ranks by
+    // their bits, and kept places per workgroup
+    int32_t* pick;
+    unsigned int* hist;
+    int2* chunk;
 };
 size_t evict_workspace_bytes(int64_t n_seq, int64_t count);
 hipError_t launch_evict(EvictArgs& a, void* workspace, hipStream_t st);
