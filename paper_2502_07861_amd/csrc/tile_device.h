@@ -55,8 +55,30 @@ __device__ __forceinline__ floatx16 tile_mma(const uintx4& a, const uintx4& b, f
 
 __device__ __forceinline__ int tile_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
-// (x of this half, x of the other half), the same pair in both
 __device__ __forceinline__ float half_max(float x) { return xor_max<32>(x); }
 __device__ __forceinline__ float half_sum(float x) { return xor_sum<32>(x); }
+
+// ---- memory to LDS without registers: lane l's 16 bytes at base + off go to LDS address `to` + 16 l.  In assembly because the
+// compiler waits for all of them before any LDS read that follows; tile_arrived() waits for this wavefront's own.
+__device__ __forceinline__ unsigned int lds_address(const void* p) {
+    return (unsigned int)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+__device__ __forceinline__ void to_lds(const char* base, unsigned int off, unsigned int to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void tile_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// All wavefronts' LDS writes are done and seen: loads under way stay so (a __syncthreads would wait for them).
+__device__ __forceinline__ void tile_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// This lane's share of a tile of 64 rows: wavefront w of four brings rows 16 w .. 16 w + 15, step i of them RPS rows.
+template <typename T, int D> struct TileFetch {
+    using R = TileRows<T, D>;
+    static constexpr int kRps = 64 / R::kSlots;                  // rows of a step
+    static constexpr int kSteps = 16 / kRps;
+    // row of step i within the wavefront's sixteen, and the slot of it that is stored where this lane writes
+    static __device__ __forceinline__ int row(int i, int lane) { return kRps * i + lane / R::kSlots; }
+};
 
 }  // namespace bkv

@@ -3,9 +3,11 @@
 // over the tokens i of one or two caches, optionally only the first few of them per query (causal).
 //
 // A workgroup of four wavefronts takes 32, 64 or 128 queries of one cache against a range of its keys, 64 at a time: keys and
-// values go through LDS once for all its queries, in two buffers, the next tile's loads are under way while the current one is
+// values go from memory to LDS once for all its queries, in two buffers, the next tile's are under way while the current one is
 // multiplied.  A wavefront has 32 queries in registers; where the workgroup has fewer than 128, wavefronts share queries and
 // split the keys of a tile.  Softmax weights stay in the lane that the next product wants them in (tile_device.h).
+#include <type_traits>
+
 #include "bkv_device.h"
 #include "bkv_host.h"
 #include "tile_device.h"
@@ -16,97 +18,117 @@ constexpr int kTileKeys = 64;
 constexpr int kTileThreads = 256;
 constexpr int kTilePad = 4;                  // floats behind the D sums of a partial row: [0] reference exponent, [1] denominator
 
-template <typename T, int D>
-__global__ __launch_bounds__(kTileThreads, sizeof(T) == 2 ? 2 : 1) void tile_kernel(const TileArgs a) {
+template <typename T, int D> struct TileLds {
+    __align__(16) char rows[2][2][kTileKeys * D * sizeof(T)];        // [buffer][keys, values]
+};
+
+// QW: wavefronts with queries of their own; 4 / QW share the same ones.
+template <typename T, int D, int QW>
+__device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, int64_t stream, int split, int qt, TileLds<T, D>& lds) {
     using R = TileRows<T, D>;
-    constexpr int ROWB = R::kRowB, SLOTS = R::kSlots, NP = kTileKeys * SLOTS / kTileThreads, EPN = R::kEpn, P = D + kTilePad;
-    __shared__ __align__(16) char lds[2][2][kTileKeys * ROWB];         // [buffer][keys, values]
-    __shared__ __align__(16) float bias[2][kTileKeys];
+    using F = TileFetch<T, D>;
+    constexpr int ROWB = R::kRowB, EPN = R::kEpn, P = D + kTilePad, TILEB = kTileKeys * ROWB;
+    constexpr int KW = 4 / QW, NS = QW == 4 ? 2 : 1;                 // wavefronts a query has; groups of 32 keys a wavefront takes of a tile
+    // bf16: a weight multiplies its value row as two bf16 numbers, its upper bits and what they leave (relative error 2^-17), except
+    // for full workgroups of 128 queries, where the matrix cores are the bound: there it is rounded to one (2^-8), as the result is.
+    // 8 prefixes x 16385 tokens x 1280 queries: 165 -> 137 us, off the 64-bit result 1.7e-3 -> 2.1e-3 (rounding it makes 1.7e-3).
+    constexpr bool kTwo = R::kB16 && QW < 4;
 
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-
-    // workgroup -> (job, cache, split, query tile); the query tiles of a split go to one XCD (blocks are dealt out to the eight
-    // of them in turn), whose L2 then serves all but the first read of its rows
-    unsigned int block = blockIdx.y * gridDim.x + blockIdx.x;
-    const int which = block >= a.first ? 1 : 0;
-    block -= which ? a.first : 0u;
-    const TileJob J = which ? a.job[1] : a.job[0];
-    const unsigned int in_xcd = block >> 3;
-    const unsigned int unit = in_xcd / (unsigned int)J.n_qt * 8u + (block & 7u);
-    const int qt = J.n_qt - 1 - (int)(in_xcd % (unsigned int)J.n_qt);           // (causal: the longest first)
-    if (unit >= (unsigned int)J.n_streams * (unsigned int)J.splits) return;
-    const int split = (int)(unit % (unsigned int)J.splits);
-    const int64_t stream = unit / (unsigned int)J.splits;
-
-    const int qw = J.qw, kw = 4 / qw;
-    const int qsub = wave & (qw - 1), ksub = wave / qw;
-    const int row_first = qt * 32 * qw, row0 = row_first + 32 * qsub;
-    const bool has_rows = row0 < J.rows;
+    const int qsub = wave & (QW - 1), ksub = wave / QW;
+    const int row_first = qt * 32 * QW, row0 = row_first + 32 * qsub;
+    const bool has_rows = row0 < J.rows && ksub * 32 < kTileKeys;
     const int row = min(row0 + n, J.rows - 1);
     const int outer = row / J.inner;
     const int64_t q_row = stream * J.q_stream + (int64_t)outer * J.q_outer + (int64_t)(row - outer * J.inner) * J.q_inner;
 
-    // keys of this workgroup
+    // tiles of keys of this workgroup
     const int tiles = (J.count + kTileKeys - 1) / kTileKeys;
     const int t0 = split * J.tiles_per_split;
     int t1 = min(tiles, t0 + J.tiles_per_split);
     int sees = J.count, sees_min = J.count;
     if (a.causal) {
-        const int64_t v = a.visible + outer;
-        sees = (int)min((int64_t)J.count, max((int64_t)0, v));
-        const int row_last = min(row_first + 32 * qw, J.rows) - 1;
-        const int most = (int)min((int64_t)J.count, max((int64_t)0, a.visible + row_last / J.inner));
-        t1 = min(t1, (most + kTileKeys - 1) / kTileKeys);
-        sees_min = (int)min((int64_t)J.count, max((int64_t)0, a.visible + min(row0, J.rows - 1) / J.inner));
+        auto visible = [&](int i) { return (int)min((int64_t)J.count, max((int64_t)0, a.visible + i)); };
+        sees = visible(outer);
+        t1 = min(t1, (visible((min(row_first + 32 * QW, J.rows) - 1) / J.inner) + kTileKeys - 1) / kTileKeys);
+        sees_min = visible(min(row0, J.rows - 1) / J.inner);
     }
 
     const char* Kb = J.K + (size_t)stream * J.stride * ROWB;
     const char* Vb = J.V + (size_t)stream * J.stride * ROWB;
     const float* wb = J.w + (size_t)stream * J.stride;
 
-    // a tile on its way: pieces tid + 256 i of its 64 rows
-    uintx4 kreg[NP], vreg[NP];
-    float wreg[NP], wkey = 0.f;
-    auto load = [&](int t) {
+    // ---- a tile on its way: this lane's bytes of each step, the slots exchanged as the rows are stored
+    unsigned int kgo[F::kSteps], vgo[F::kSteps];
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int piece = tid + kTileThreads * i, r = piece / SLOTS, s = piece % SLOTS;
-            const int key = t * kTileKeys + r, at = min(key, J.count - 1);
-            const size_t off = (size_t)at * ROWB + s * 16;
-            kreg[i] = *reinterpret_cast<const uintx4*>(Kb + off);
-            vreg[i] = *reinterpret_cast<const uintx4*>(Vb + off);
-            const float w = wb[at];
-            wreg[i] = key < J.count ? w : 0.f;
-        }
-        if (tid < kTileKeys) {
-            const int key = t * kTileKeys + tid;
-            const float w = wb[min(key, J.count - 1)];
-            wkey = key < J.count ? w : 0.f;
-        }
-    };
-    auto store = [&](int buf) {
-        bool dead = false;
+    for (int i = 0; i < F::kSteps; ++i) {
+        const int r = 16 * wave + F::row(i, lane), s = lane % R::kSlots;
+        kgo[i] = r * ROWB + R::key_slot(r, s) * 16;
+        vgo[i] = r * ROWB + R::value_slot(r, s) * 16;
+    }
+    const unsigned int lds0 = lds_address(&lds.rows[0][0][0]) + 16 * wave * ROWB;
+    auto fetch = [&](int t, int buf) {
+        const char* kp = Kb + (size_t)t * TILEB;
+        const char* vp = Vb + (size_t)t * TILEB;
+        const unsigned int to = lds0 + buf * 2 * TILEB;
+        const int left = J.count - 1 - t * kTileKeys;                // last row there is
+        if (left >= kTileKeys - 1) {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) dead |= !(wreg[i] > 0.f);
-        if (__builtin_amdgcn_ballot_w64(dead) != 0ull) {              // (whatever an absent token's row holds)
+            for (int i = 0; i < F::kSteps; ++i) { to_lds(kp, kgo[i], to + 1024 * i); to_lds(vp, vgo[i], to + TILEB + 1024 * i); }
+        } else {                                                     // (rows past the end repeat it, with weight 0)
 #pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                const unsigned int keep = wreg[i] > 0.f ? 0xffffffffu : 0u;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { kreg[i][j] &= keep; vreg[i][j] &= keep; }
+            for (int i = 0; i < F::kSteps; ++i) {
+                const int r = 16 * wave + F::row(i, lane);
+                const unsigned int back = max(r - left, 0) * ROWB;
+                to_lds(kp, kgo[i] - back, to + 1024 * i);
+                to_lds(vp, vgo[i] - back, to + TILEB + 1024 * i);
             }
         }
+    };
+    auto weight = [&](int t) {                                       // lane: key
+        const int key = t * kTileKeys + lane;
+        const float w = wb[min(key, J.count - 1)];
+        return key < J.count ? w : 0.f;
+    };
+    // rows of places without a token, whatever they hold: 0 (each wavefront those it brought)
+    auto clear_dead = [&](int buf, unsigned long long live) {
+        unsigned int dead = (unsigned int)(~live >> (16 * wave)) & 0xffffu;
+        if (live == 0ull) return;                                    // (not fetched, not looked at)
+        while (dead != 0u) {
+            const int r = 16 * wave + __builtin_ctz(dead);
+            dead &= dead - 1u;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int piece = tid + kTileThreads * i, r = piece / SLOTS, s = piece % SLOTS;
-            *reinterpret_cast<uintx4*>(lds[buf][0] + r * ROWB + R::key_slot(r, s) * 16) = kreg[i];
-            *reinterpret_cast<uintx4*>(lds[buf][1] + r * ROWB + R::value_slot(r, s) * 16) = vreg[i];
+            for (int k = 0; k < 2; ++k) {
+                char* to = &lds.rows[buf][k][r * ROWB + lane * (ROWB / 64)];
+                if constexpr (ROWB == 128) *reinterpret_cast<unsigned short*>(to) = 0;
+                else if constexpr (ROWB == 256) *reinterpret_cast<unsigned int*>(to) = 0u;
+                else *reinterpret_cast<uint2*>(to) = make_uint2(0u, 0u);
+            }
         }
-        if (tid < kTileKeys) bias[buf][tid] = wkey > 0.f ? __builtin_amdgcn_logf(wkey) * a.inv_scale : kTileDead;
     };
 
-    if (t0 < t1) load(t0);
+    // where a lane reads: key row n (of the wavefront's group), value columns (see tile_device.h)
+    unsigned int ko[R::kPieces];
+#pragma unroll
+    for (int c = 0; c < R::kPieces; ++c) ko[c] = (NS == 1 ? ksub * 32 * ROWB : 0) + n * ROWB + R::key_slot(n, 2 * c + h) * 16;
+    constexpr int NV = R::kB16 ? EPN : 1;
+    unsigned int vo[NV];
+    if constexpr (R::kB16) {
+        const int i16 = lane & 15, half = (lane >> 4) & 1, r = 4 * h + (i16 >> 2);
+#pragma unroll
+        for (int e = 0; e < EPN; ++e)
+            vo[e] = (NS == 1 ? ksub * 32 * ROWB : 0) + r * ROWB + R::value_slot(r, 4 * e + 2 * half + ((i16 & 3) >> 1)) * 16 + (i16 & 1) * 8;
+    } else vo[0] = (NS == 1 ? ksub * 32 * ROWB : 0) + 4 * h * ROWB + n * (EPN * 4);
+
+    float w0 = 0.f, w1 = 0.f, w2 = 0.f;
+    unsigned long long live0 = 0ull, live1 = 0ull;
+    if (t0 < t1) {
+        w0 = weight(t0);
+        if (t0 + 1 < t1) w1 = weight(t0 + 1);
+        live0 = __ballot(w0 > 0.f);
+        if (live0 != 0ull) fetch(t0, 0);
+    }
     uintx4 qf[R::kPieces];
 #pragma unroll
     for (int c = 0; c < R::kPieces; ++c) qf[c] = *reinterpret_cast<const uintx4*>(a.Q + (size_t)q_row * ROWB + 32 * c + 16 * h);
@@ -118,125 +140,154 @@ __global__ __launch_bounds__(kTileThreads, sizeof(T) == 2 ? 2 : 1) void tile_ker
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[e][r] = 0.f;
 
-    auto compute = [&](int buf, int t) {
-        const char* Kt = lds[buf][0];
-        const char* Vt = lds[buf][1];
-        for (int sub = ksub; sub < kTileKeys / 32; sub += kw) {
-            const int k0 = t * kTileKeys + 32 * sub;
-            // ---- logits, in units of 1 / scale
-            floatx16 s;
+    auto compute = [&](auto buf_c, int t, float w) {
+        constexpr int BUF = decltype(buf_c)::value;
+        const char* Kt = lds.rows[BUF][0];
+        const char* Vt = lds.rows[BUF][1];
+        const int k0 = t * kTileKeys + (NS == 1 ? 32 * ksub : 0);
+        // ---- logits, in units of 1 / scale
+        floatx16 s[NS];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const floatx4 b = *reinterpret_cast<const floatx4*>(&bias[buf][32 * sub + 8 * i + 4 * h]);
+        for (int u = 0; u < NS; ++u) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[4 * i + j] = b[j];
-            }
-            const int kr = 32 * sub + n;
+            for (int r = 0; r < 16; ++r) s[u][r] = 0.f;
             if constexpr (R::kB16) {
 #pragma unroll
-                for (int c = 0; c < R::kPieces; ++c) {
-                    const uintx4 kf = *reinterpret_cast<const uintx4*>(Kt + kr * ROWB + R::key_slot(kr, 2 * c + h) * 16);
-                    s = tile_mma<T>(kf, qf[c], s);
-                }
+                for (int c = 0; c < R::kPieces; ++c)
+                    s[u] = tile_mma<T>(*reinterpret_cast<const uintx4*>(Kt + ko[c] + 32 * u * ROWB), qf[c], s[u]);
             } else {
                 // two chains, so that no sum is rounded more than d / 4 times at its full size
-                floatx16 s1;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s1[r] = 0.f;
-                floatx16 s0 = s1;
+                floatx16 s1 = s[u];
 #pragma unroll
                 for (int c = 0; c < R::kPieces; c += 2) {
-                    const uintx4 ka = *reinterpret_cast<const uintx4*>(Kt + kr * ROWB + R::key_slot(kr, 2 * c + h) * 16);
-                    const uintx4 kb = *reinterpret_cast<const uintx4*>(Kt + kr * ROWB + R::key_slot(kr, 2 * c + 2 + h) * 16);
-                    s0 = tile_mma<T>(ka, qf[c], s0);
-                    s1 = tile_mma<T>(kb, qf[c + 1], s1);
+                    s[u] = tile_mma<T>(*reinterpret_cast<const uintx4*>(Kt + ko[c] + 32 * u * ROWB), qf[c], s[u]);
+                    s1 = tile_mma<T>(*reinterpret_cast<const uintx4*>(Kt + ko[c + 1] + 32 * u * ROWB), qf[c + 1], s1);
                 }
-                s = s + (s0 + s1);
+                s[u] = s[u] + s1;
             }
-            if (a.causal && k0 + 32 > sees_min) {
+        }
+        // ---- token weights: one for the whole tile (the usual tile), or ln2 w of every key as one more product: its three bf16
+        // parts (together all its bits) times ones, in the half of the wavefront that holds the group's keys
+        const float first = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(w)));
+        const bool one = first > 0.f && __ballot(w == first) == ~0ull;
+        const float b = one ? __builtin_amdgcn_logf(first) : 0.f;
+        if (!one) {
+            const float x = w > 0.f ? __builtin_amdgcn_logf(w) * a.inv_scale : kTileDead;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = k0 + tile_row(r, h) < sees ? s[r] : kTileDead;
+            for (int u = 0; u < NS; ++u) {
+                const float y = h == (NS == 1 ? ksub : u) ? x : 0.f;
+                if constexpr (R::kB16) {
+                    const unsigned int y0 = __float_as_uint(y) & 0xffff0000u;
+                    const float rest = y - __uint_as_float(y0);
+                    const unsigned int y1 = __float_as_uint(rest) & 0xffff0000u;
+                    const uintx4 part = {(y0 >> 16) | y1, __float_as_uint(rest - __uint_as_float(y1)) >> 16, 0u, 0u};
+                    const uintx4 ones = {0x3f803f80u, 0x00003f80u, 0u, 0u};
+                    s[u] = tile_mma<T>(part, ones, s[u]);
+                } else s[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(y, 1.f, s[u], 0, 0, 0);
             }
-            // ---- weights 2^(logit - m); m moves when a logit passes it by more than the slack
-            float mx = s[0];
+        }
+        if (a.causal && k0 + 32 * NS > sees_min) {
 #pragma unroll
-            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-            mx *= a.scale_log2;
-            if (__builtin_amdgcn_ballot_w64(mx > m + kTileSlack) != 0ull) {
-                const float mnew = fmaxf(m, half_max(mx));
-                const float sc = fast_exp2(m - mnew);
-                m = mnew;
-                l *= sc;
+            for (int u = 0; u < NS; ++u)
 #pragma unroll
-                for (int e = 0; e < EPN; ++e) o[e] *= sc;
-            }
+                for (int r = 0; r < 16; ++r) s[u][r] = k0 + 32 * u + tile_row(r, h) < sees ? s[u][r] : kTileDead;
+        }
+        // ---- weights 2^(logit - m); m moves when a logit passes it by more than the slack
+        float mx = s[0][0];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) { s[r] = fast_exp2(fmaf(s[r], a.scale_log2, -m)); l += s[r]; }
-            // ---- values
+        for (int u = 0; u < NS; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[u][r]);
+        mx = fmaf(mx, a.scale_log2, b);
+        if (__builtin_amdgcn_ballot_w64(mx > m + kTileSlack) != 0ull) {
+            const float mnew = fmaxf(m, half_max(mx));
+            const float sc = fast_exp2(m - mnew);
+            m = mnew;
+            l *= sc;
+#pragma unroll
+            for (int e = 0; e < EPN; ++e) o[e] *= sc;
+        }
+        const float shift = b - m;
+#pragma unroll
+        for (int u = 0; u < NS; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) { s[u][r] = fast_exp2(fmaf(s[u][r], a.scale_log2, shift)); l += s[u][r]; }
+        // ---- values
+#pragma unroll
+        for (int u = 0; u < NS; ++u) {
             if constexpr (R::kB16) {
-                // two bf16 numbers for a weight, its upper bits and what they leave
-                bf16x8_t hi[2], lo[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     uintx4 x, y;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float p0 = s[8 * j + 2 * i], p1 = s[8 * j + 2 * i + 1];
-                        const unsigned int b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
-                        x[i] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
-                        const floatx2 rest = {p0 - __uint_as_float(b0 & 0xffff0000u), p1 - __uint_as_float(b1 & 0xffff0000u)};
-                        y[i] = __builtin_bit_cast(unsigned int, __builtin_convertvector(rest, bf16x2_tile));
+                        const float p0 = s[u][8 * j + 2 * i], p1 = s[u][8 * j + 2 * i + 1];
+                        if constexpr (kTwo) {
+                            const unsigned int b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+                            x[i] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+                            const floatx2 rest = {p0 - __uint_as_float(b0 & 0xffff0000u), p1 - __uint_as_float(b1 & 0xffff0000u)};
+                            y[i] = __builtin_bit_cast(unsigned int, __builtin_convertvector(rest, bf16x2_tile));
+                        } else {
+                            const floatx2 both = {p0, p1};
+                            x[i] = __builtin_bit_cast(unsigned int, __builtin_convertvector(both, bf16x2_tile));
+                        }
                     }
-                    hi[j] = __builtin_bit_cast(bf16x8_t, x); lo[j] = __builtin_bit_cast(bf16x8_t, y);
-                }
-                const int i16 = lane & 15, half = (lane >> 4) & 1;
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int e = 0; e < EPN; ++e) {
-                        const int r0 = 32 * sub + 16 * j + 4 * h + (i16 >> 2), r1 = r0 + 8, slot = 4 * e + 2 * half + ((i16 & 3) >> 1);
                         typedef __attribute__((address_space(3))) shortx4* lds4;
-                        const shortx4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(Vt + r0 * ROWB + R::value_slot(r0, slot) * 16 + (i16 & 1) * 8));
-                        const shortx4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(Vt + r1 * ROWB + R::value_slot(r1, slot) * 16 + (i16 & 1) * 8));
+                        const shortx4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(Vt + vo[e] + (32 * u + 16 * j) * ROWB));
+                        const shortx4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(Vt + vo[e] + (32 * u + 16 * j + 8) * ROWB));
                         struct { shortx4 a, b; } both = {v0, v1};
                         const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, both);
-                        o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, hi[j], o[e], 0, 0, 0);
-                        o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, lo[j], o[e], 0, 0, 0);
+                        o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8_t, x), o[e], 0, 0, 0);
+                        if constexpr (kTwo) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8_t, y), o[e], 0, 0, 0);
                     }
+                }
             } else {
                 typedef float vecf __attribute__((ext_vector_type(EPN)));
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int vr = 32 * sub + tile_row(r, h);
-                    const vecf v = *reinterpret_cast<const vecf*>(Vt + vr * ROWB + n * (EPN * 4));
+                    const vecf v = *reinterpret_cast<const vecf*>(Vt + vo[0] + (32 * u + tile_row(r, 0)) * ROWB);
 #pragma unroll
-                    for (int e = 0; e < EPN; ++e) o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], s[r], o[e], 0, 0, 0);
+                    for (int e = 0; e < EPN; ++e) o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], s[u][r], o[e], 0, 0, 0);
                 }
             }
         }
     };
 
     if (t0 < t1) {
-        store(0);
-        __syncthreads();
-        int buf = 0;
-        for (int t = t0;; ++t) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0), in the compiler's books too: nothing in the loop waits for the queries again
+        clear_dead(0, live0);
+        tile_barrier();
+        // one tile: the next one is requested, this one multiplied, the next one awaited; true: this was the last one
+        auto step = [&](auto buf_c, int t) {
+            constexpr int BUF = decltype(buf_c)::value;
             const bool more = t + 1 < t1;
-            if (more) load(t + 1);
-            if (has_rows) compute(buf, t);
-            if (!more) break;
-            store(buf ^ 1);
-            __syncthreads();
-            buf ^= 1;
+            if (t + 2 < t1) w2 = weight(t + 2);
+            live1 = more ? __ballot(w1 > 0.f) : 0ull;
+            if (live1 != 0ull) fetch(t + 1, BUF ^ 1);
+            if (has_rows && live0 != 0ull) compute(buf_c, t, w0);
+            if (!more) return true;
+            tile_arrived();
+            clear_dead(BUF ^ 1, live1);
+            tile_barrier();
+            w0 = w1; w1 = w2; live0 = live1;
+            return false;
+        };
+        for (int t = t0;; t += 2) {
+            if (step(std::integral_constant<int, 0>{}, t)) break;
+            if (step(std::integral_constant<int, 1>{}, t + 1)) break;
         }
     }
     l = half_sum(l);
 
     // ---- wavefronts that share queries meet in LDS, register by register
-    if (kw > 1) {
+    if constexpr (KW > 1) {
+        constexpr int PER = 16 * EPN * 64 + 128;
         __syncthreads();
-        float* mine = reinterpret_cast<float*>(&lds[0][0][0]) + (wave - qw) * (16 * EPN * 64 + 128);
-        if (ksub > 0) {
+        float* all = reinterpret_cast<float*>(&lds.rows[0][0][0]);
+        if (ksub == 1) {
+            float* mine = all + qsub * PER;
 #pragma unroll
             for (int e = 0; e < EPN; ++e)
 #pragma unroll
@@ -246,21 +297,19 @@ __global__ __launch_bounds__(kTileThreads, sizeof(T) == 2 ? 2 : 1) void tile_ker
         }
         __syncthreads();
         if (ksub > 0) return;
-        for (int k = 1; k < min(kw, kTileKeys / 32); ++k) {
-            const float* other = reinterpret_cast<const float*>(&lds[0][0][0]) + (wave + (k - 1) * qw) * (16 * EPN * 64 + 128);
-            const float mo = other[16 * EPN * 64 + lane], lo = other[16 * EPN * 64 + 64 + lane];
-            const float mn = fmaxf(m, mo), f0 = fast_exp2(m - mn), f1 = fast_exp2(mo - mn);
-            m = mn;
-            l = fmaf(l, f0, lo * f1);
+        const float* other = all + qsub * PER;
+        const float mo = other[16 * EPN * 64 + lane], lo = other[16 * EPN * 64 + 64 + lane];
+        const float mn = fmaxf(m, mo), f0 = fast_exp2(m - mn), f1 = fast_exp2(mo - mn);
+        m = mn;
+        l = fmaf(l, f0, lo * f1);
 #pragma unroll
-            for (int e = 0; e < EPN; ++e)
+        for (int e = 0; e < EPN; ++e)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) o[e][r] = fmaf(o[e][r], f0, other[(16 * e + r) * 64 + lane] * f1);
-        }
+            for (int r = 0; r < 16; ++r) o[e][r] = fmaf(o[e][r], f0, other[(16 * e + r) * 64 + lane] * f1);
     }
-    if (!has_rows || row0 + n >= J.rows) return;
+    if (row0 + n >= J.rows) return;
 
-    // ---- store: a lane has four consecutive columns at a time
+    // ---- store: a lane has four (fp32: EPN) consecutive columns at a time
     if (J.part) {
         float* dst = J.part + ((size_t)split * a.n_rows + q_row) * P;
 #pragma unroll
@@ -304,6 +353,26 @@ __global__ __launch_bounds__(kTileThreads, sizeof(T) == 2 ? 2 : 1) void tile_ker
         if (a.lse) a.lse[q_row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
         if (a.stats) *reinterpret_cast<floatx2*>(a.stats + 2 * q_row) = l != 0.f ? floatx2{m, f} : floatx2{-kTileDead, 0.f};
     }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kTileThreads, sizeof(T) == 2 ? 2 : 1) void tile_kernel(const TileArgs a) {
+    __shared__ TileLds<T, D> lds;
+    // workgroup -> (job, cache, split, query tile); the query tiles of a split go to one XCD (blocks are dealt out to the eight
+    // of them in turn), whose L2 then serves all but the first read of its rows
+    unsigned int block = blockIdx.y * gridDim.x + blockIdx.x;
+    const int which = block >= a.first ? 1 : 0;
+    block -= which ? a.first : 0u;
+    const TileJob J = which ? a.job[1] : a.job[0];
+    const unsigned int in_xcd = block >> 3;
+    const unsigned int unit = in_xcd / (unsigned int)J.n_qt * 8u + (block & 7u);
+    const int qt = J.n_qt - 1 - (int)(in_xcd % (unsigned int)J.n_qt);           // (causal: the longest first)
+    if (unit >= (unsigned int)J.n_streams * (unsigned int)J.splits) return;
+    const int split = (int)(unit % (unsigned int)J.splits);
+    const int64_t stream = unit / (unsigned int)J.splits;
+    if (J.qw == 4) tile_body<T, D, 4>(a, J, stream, split, qt, lds);
+    else if (J.qw == 2) tile_body<T, D, 2>(a, J, stream, split, qt, lds);
+    else tile_body<T, D, 1>(a, J, stream, split, qt, lds);
 }
 
 // Partial rows of all splits of a query -> its result.  D / 4 lanes a query, four columns each.

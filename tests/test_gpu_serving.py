@@ -2,7 +2,8 @@
 
 Tolerances, per output element.  u = 2^-24 is half a step of fp32, n the tokens a query runs over, p their softmax weights:
   logit    |error| <= dl = (d + 8) u max_j sum_c |k_jc q_c| / sqrt d, plus 4 u of its own size and of the reference's (rounded products, the scale)
-  weight   relative 2 dl (its own logit and the denominator's) + (n + 64) u (the sums) + 2^-16 (exp2; bf16: the two-number weights)
+  weight   relative 2 dl (its own logit and the denominator's) + (n + 64) u (the sums) + 2^-16 (exp2; bf16: the two-number weights);
+           + 2^-8 in the output of bf16 caches with more than 64 queries, whose weights are rounded to one bf16 number (half a step)
   out      that, times sum_j p_j |v_j|; and the rounding of the result: bf16 2^-8, fp32 u, relative
   lse      dl + (n + 64) u + 4 u |lse|
   mass     sum over the queries of p times the weights' bound, + 4 u of the result and (rows) u of the sum
@@ -68,8 +69,9 @@ def _attention(Q, K, V, w, sees=None):
     return P @ V, lse, P, 2 * dl + (K.shape[0] + 64) * U + 2.0 ** -16, dl, P @ V.abs()
 
 
-def _check_out(out, lse, ref, dtype, n, what):
+def _check_out(out, lse, ref, dtype, n, what, rows=1):
     z, l, P, rel, dl, zabs = ref
+    rel = rel + (2.0 ** -8 if dtype == BF16 and rows > 64 else 0.0)
     out, z = out.double().reshape(z.shape), z
     half = 2.0 ** -8 if dtype == BF16 else U
     tol = rel[:, None] * zabs + half * z.abs() * (1 + rel[:, None]) + 1e-30
@@ -102,7 +104,7 @@ def test_prefix(bk, dtype, d, n_pre, fan, g, nq, cp, cs):
     for s in range(0, n_seq, max(1, n_seq // 40)):
         k = s % n_pre
         K, V, w = (torch.cat([a[k, :cp], b[s, :cs]]) for a, b in zip(pre, own))
-        _check_out(out[s], lse[s], _attention(Q[s].reshape(-1, d), K, V, w), dtype, cp + cs, "sequence %d" % s)
+        _check_out(out[s], lse[s], _attention(Q[s].reshape(-1, d), K, V, w), dtype, cp + cs, "sequence %d" % s, fan * g * nq)
     again, lse2 = bk.attend_prefix(p, pre, own, Q, count_prefix=cp, count_own=cs)
     assert torch.equal(out.view(torch.int16 if dtype == BF16 else torch.int32), again.view(torch.int16 if dtype == BF16 else torch.int32))
     assert torch.equal(lse, lse2)
@@ -166,7 +168,7 @@ def test_mass(bk, dtype, d, n_seq, count, g, nq, visible, decay):
     sees = None if visible is None else (visible + torch.arange(nq, device="cuda")).repeat(g)
     for s in range(0, n_seq, max(1, n_seq // 20)):
         ref = _attention(Q[s].reshape(-1, d), K[s, :count], V[s, :count], w[s, :count], sees)
-        _check_out(out[s], lse[s], ref, dtype, count, "sequence %d" % s)
+        _check_out(out[s], lse[s], ref, dtype, count, "sequence %d" % s, g * nq)
         _check_mass(into[s], before[s], decay, ref, count, g * nq, "sequence %d" % s)
     # in place, and the same bits
     out2, _, got = bk.attend_mass(p, K, V, w, Q, mass, count=count, visible=visible, decay=decay, mass_out=mass, lse=False)
