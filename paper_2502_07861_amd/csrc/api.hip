@@ -491,8 +491,11 @@ size_t bkv_attend_mass_workspace_bytes(const bkv_params* p, int64_t n_seq, int64
     if (check_queries(p, n_seq, g, nq) || count < 0) return 0;
     const int64_t n_q = (int64_t)g * nq;
     const int splits = bkv::tile_most_splits(n_seq, n_q);
-    return align_up((size_t)n_seq * n_q * 8, 256) + (splits > 1 ? align_up(bkv::tile_part_bytes(p->d, n_seq * n_q, splits), 256) : 0) +
-           bkv::mass_part_bytes();
+    const size_t tiles = align_up((size_t)n_seq * n_q * 8, 256) + (splits > 1 ? align_up(bkv::tile_part_bytes(p->d, n_seq * n_q, splits), 256) : 0) +
+                         bkv::mass_part_bytes();
+    if (!bkv::attend_keeps_logits(row_bytes(p), n_q)) return tiles;
+    const size_t few = align_up(bkv::attend_mass_bytes(p->dtype, p->d, n_seq, count, (int)n_q), 256);
+    return few > tiles ? few : tiles;                  // (which of the two a call takes depends on `visible` too)
 }
 
 int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const float* w, int64_t n_seq, int64_t count,
@@ -514,6 +517,17 @@ int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const
     if (mass_in != mass_out && overlap(mass_in, m_bytes, mass_out, m_bytes)) return BKV_EINVAL;
     if (overlap(w, m_bytes, mass_out, m_bytes)) return BKV_EINVAL;
     if (!workspace || ws_bytes < bkv_attend_mass_workspace_bytes(p, n_seq, count, g, nq) || !aligned16(workspace)) return BKV_EWORKSPACE;
+    if (decay == 0.f) mass_in = nullptr;
+    if (visible >= count && bkv::attend_keeps_logits(row_bytes(p), n_q)) {
+        bkv::AttendArgs a;
+        memset(&a, 0, sizeof(a));
+        a.set[0].K = (const char*)K_c; a.set[0].V = (const char*)V_c; a.set[0].w = w;
+        a.set[0].stride = stride_tokens; a.set[0].count = count;
+        a.Q = (const char*)Q; a.out = (char*)out; a.lse_out = lse_out; a.n_seq = n_seq; a.n_q = n_q;
+        a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)p->d));
+        const hipError_t e = bkv::launch_attend_mass(p->dtype, p->d, a, bkv::AttendMass{mass_in, mass_out, decay}, workspace, st);
+        return e == hipSuccess ? BKV_OK : hip_fail(e);
+    }
     // rows of a cache in the order of their positions, its query heads next to each other
     bkv::TileArgs a;
     tile_common(a, p, Q, out, lse_out, n_seq * n_q);
@@ -532,9 +546,8 @@ int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const
     if (splits > 1) ws += align_up(bkv::tile_part_bytes(p->d, n_seq * n_q, splits), 256);
     bkv::MassArgs b;
     memset(&b, 0, sizeof(b));
-    b.K = (const char*)K_c; b.w = w; b.Q = (const char*)Q; b.stats = a.stats; b.mass = decay > 0.f ? mass_in : nullptr; b.mass_out = mass_out;
-    b.stride = stride_tokens; b.n_seq = n_seq; b.q_stream = j.q_stream; b.q_outer = j.q_outer; b.q_inner = j.q_inner;
-    b.visible = a.visible; b.count = (int32_t)count; b.rows = n_q; b.inner = g; b.causal = a.causal;
+    b.K = (const char*)K_c; b.w = w; b.Q = (const char*)Q; b.stats = a.stats; b.mass = mass_in; b.mass_out = mass_out;
+    b.stride = stride_tokens; b.n_seq = n_seq; b.visible = a.visible; b.count = (int32_t)count; b.rows = n_q; b.nq = nq; b.causal = a.causal;
     b.scale_log2 = a.scale_log2; b.inv_scale = a.inv_scale; b.decay = decay; b.part = (float*)ws;
     e = bkv::launch_mass(p->dtype, p->d, b, st);
     return e == hipSuccess ? BKV_OK : hip_fail(e);

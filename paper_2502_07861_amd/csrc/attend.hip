@@ -180,7 +180,8 @@ __device__ __forceinline__ void merge_rows(const float* part, size_t sstride, in
 // values after O^T), so that about 12 KB per wavefront are under way at any time.
 // STREAM: K and V are read past the caches (see attend_streams).
 // ONE: a workgroup takes both sets of a sequence as a whole, nothing is merged behind it (see attend_in_one).
-template <typename T, int D, int NQT, int W, bool STREAM = false, bool ONE = false>
+// LOGITS: the logits of every group that holds a token go to memory, value rows of absent tokens count as zeros whatever they hold.
+template <typename T, int D, int NQT, int W, bool STREAM = false, bool ONE = false, bool LOGITS = false>
 __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
     constexpr bool B16 = sizeof(T) == 2;
     constexpr int ROWB = D * (int)sizeof(T);
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
     // The reference m moves only when a logit passes it by more than kSlack (then to the largest one, for all lanes of the
     // query): the weights are floating-point numbers, so a reference that is 2^6 too small costs nothing.
     bf16x8_t pb[NQT], pl[NQT];
-    auto softmax = [&](const float (&w)[VR]) {
+    auto softmax = [&](const float (&w)[VR], int64_t group) {
         float bias[VR];
         bool dead = false;
 #pragma unroll
@@ -435,6 +436,24 @@ __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
             for (int t = 0; t < NQT; ++t)
 #pragma unroll
                 for (int x = 0; x < VR; ++x) s[t][x >> 2][x & 3] = w[x] > 0.f ? s[t][x >> 2][x & 3] : 0.f;
+            if constexpr (LOGITS) {
+#pragma unroll
+                for (int x = 0; x < VR; ++x)
+#pragma unroll
+                    for (int c = 0; c < VD; ++c) vf[x][c] = w[x] > 0.f ? vf[x][c] : 0u;
+            }
+        }
+        if constexpr (LOGITS) {
+            if (n < a.n_q) {
+                float* to = a.logits + ((((size_t)seq * groups + group) * NT) * a.n_q + n) * 16 + 4 * kg;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    floatx4 x;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] = fmaf(s[0][t][r], a.scale_log2, bias[4 * t + r]);
+                    *reinterpret_cast<floatx4*>(to + 16 * t * a.n_q) = x;
+                }
+            }
         }
         bool grew = false;
         float mx[NQT];
@@ -526,7 +545,7 @@ __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
             if (more && gn + W < gf) load_w(w1, gn + W);
             qk();
             if (more) load_k(gn);
-            softmax(wc);
+            softmax(wc, g);
             if (has_v) {
                 pv();
                 if (more) load_v(gn);
@@ -545,7 +564,7 @@ __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
             if (more) { if (x < full) load_w(w0, x); else load_w_end(w0); }
             qk();
             if (more) { if (x < full) load_k(x); else load_k_end(); }
-            softmax(wc);
+            softmax(wc, 0);
             if (has_v) {
                 pv();
                 if (more) { if (x < full) load_v(x); else load_v_end(); }
@@ -559,7 +578,7 @@ __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
         load_w_end(wt);
         if (has_v) load_v_end();
         qk();
-        softmax(wt);
+        softmax(wt, full);
         if (has_v) pv();
     }
 #pragma unroll
@@ -628,6 +647,9 @@ __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
         if (ns == 1) {                          // the whole range was one split: normalise and store
             store4<T>(a.out, (row0 + q) * D + col, acc * (L > 0.f ? 1.f / L : 0.f));
             if (col == 0 && a.lse_out) a.lse_out[row0 + q] = L > 0.f ? log2_or(L, M) * 0.6931471805599453f : -INFINITY;
+            if constexpr (LOGITS) {
+                if (col == 0) *reinterpret_cast<floatx2*>(a.stats + 2 * (row0 + q)) = floatx2{M, L > 0.f ? 1.f / L : 0.f};
+            }
         } else {
             float* dst = part + split * sstride + q * P;
             if (has_v) { put2(dst + col, acc[0], acc[1]); put2(dst + col + 2, acc[2], acc[3]); }
@@ -657,6 +679,78 @@ __global__ __launch_bounds__(kMergeThreads) void attend_merge_kernel(const Atten
     const size_t sstride = (size_t)a.rows * (D + kRowPad);
     const float* part = a.partial + ((size_t)seq * a.n_qg + qg) * ns * sstride + (size_t)(q - qg * rq) * (D + kRowPad);
     merge_rows<T, D, kMergeThreads>(part, sstride, 1, a.ns[0], a.ns[1], a.out, a.lse_out, (size_t)seq * a.n_q + q, red);
+}
+
+// Behind a pass with its logits kept: the first merge_blocks workgroups merge a query's splits each (none where there is one), each of
+// the others has 1024 places of a sequence, mass_out = decay mass + sum_q 2^(logit - m_q) / l_q.  It puts m and l of the sequence's
+// queries together from the partial rows by itself, so that one launch does both.
+template <typename T, int D>
+__global__ __launch_bounds__(kMergeThreads) void attend_mass_kernel(const AttendArgs a, const AttendMass b, uint32_t merge_blocks) {
+    constexpr int P = D + kRowPad, KEYS = sizeof(T) == 2 ? 32 : 16;
+    __shared__ __align__(16) float red[kMergeThreads * 8];
+    uint32_t block = blockIdx.y * gridDim.x + blockIdx.x;
+    const int ns = a.ns[0];
+    const size_t sstride = (size_t)a.rows * P;
+    if (block < merge_blocks) {
+        const int64_t seq = block / (uint32_t)a.n_q;
+        const int q = (int)(block % (uint32_t)a.n_q);
+        merge_rows<T, D, kMergeThreads>(a.partial + (size_t)seq * ns * sstride + (size_t)q * P, sstride, 1, ns, 0, a.out, a.lse_out, (size_t)seq * a.n_q + q, red);
+        return;
+    }
+    block -= merge_blocks;
+    const AttendSet& S = a.set[0];
+    const uint32_t chunks = (uint32_t)((S.count + 4 * kMergeThreads - 1) / (4 * kMergeThreads));
+    const int64_t seq = block / chunks;
+    if (seq >= a.n_seq) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    floatx2* st = reinterpret_cast<floatx2*>(red);
+    for (int q = wave; q < a.n_q; q += kMergeThreads / 64) {
+        floatx2 ml;
+        if (ns > 1) {
+            const float* part = a.partial + (size_t)seq * ns * sstride + (size_t)q * P + D;
+            float m = kNeg, l = 0.f;
+            for (int s = lane; s < ns; s += 64) {
+                const floatx2 x = *reinterpret_cast<const floatx2*>(part + s * sstride);
+                const float mn = fmaxf(m, x[0]);
+                l = fmaf(l, fast_exp2(m - mn), x[1] * fast_exp2(x[0] - mn));
+                m = mn;
+            }
+            const float all = wave_max(m);
+            l = wave_sum(l * fast_exp2(m - all));
+            ml = floatx2{all, l > 0.f ? 1.f / l : 0.f};
+        } else ml = *reinterpret_cast<const floatx2*>(a.stats + 2 * ((size_t)seq * a.n_q + q));
+        if (lane == 0) st[q] = ml;
+    }
+    __syncthreads();
+    const int64_t key = 4 * ((int64_t)(block % chunks) * kMergeThreads + threadIdx.x);
+    if (key >= S.count) return;
+    const float* lg = a.logits + ((size_t)seq * ((S.count + KEYS - 1) / KEYS * (KEYS / 16)) + key / 16) * a.n_q * 16 + key % 16;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int q = 0; q < a.n_q; ++q) {
+        const floatx4 x = *reinterpret_cast<const floatx4*>(lg + q * 16);
+        const floatx2 ml = st[q];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(fast_exp2(x[e] - ml[0]), ml[1], acc[e]);
+    }
+    // (groups without a token have not been written: what is there is not looked at)
+    const size_t at = (size_t)seq * S.stride + key;
+    if (key + 4 <= S.count) {
+        const floatx4_u w = *reinterpret_cast<const floatx4_u*>(S.w + at);
+        floatx4_u old = {0.f, 0.f, 0.f, 0.f}, out;
+        if (b.mass) old = *reinterpret_cast<const floatx4_u*>(b.mass + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float x = w[e] > 0.f ? acc[e] : 0.f;
+            out[e] = b.mass ? fmaf(b.decay, old[e], x) : x;
+        }
+        *reinterpret_cast<floatx4_u*>(b.mass_out + at) = out;
+    } else {
+        for (int e = 0; key + e < S.count; ++e) {
+            const float x = S.w[at + e] > 0.f ? acc[e] : 0.f;
+            b.mass_out[at + e] = b.mass ? fmaf(b.decay, b.mass[at + e], x) : x;
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -775,6 +869,53 @@ static hipError_t launch_attend_t(const AttendArgs& a, const AttendPlan& p, hipS
     if (e != hipSuccess || p.ns[0] + p.ns[1] == 1 || p.fused) return e;
     return launch_timed(kProfAttendMerge, a.n_seq * a.n_q, attend_merge_kernel<T, D>, dim3(a.n_q, (unsigned)a.n_seq), dim3(kMergeThreads), 0, st,
                         a, 16 * p.nqt);
+}
+
+// Keeping a query's logits costs 8 bytes a token, written and read, reading the keys again their row.
+bool attend_keeps_logits(int row_bytes, int64_t n_q) { return n_q <= 16 && 16 * n_q <= row_bytes; }
+static size_t mass_align(size_t n) { return (n + 255) / 256 * 256; }
+static size_t logit_bytes(int dtype, int64_t n_seq, int64_t count, int n_q) {
+    const int keys = dtype == BKV_BF16 ? 32 : 16;
+    return (size_t)n_seq * n_q * ((count + keys - 1) / keys * keys) * sizeof(float);
+}
+size_t attend_mass_bytes(int dtype, int d, int64_t n_seq, int64_t count, int n_q) {
+    return mass_align(logit_bytes(dtype, n_seq, count, n_q)) + mass_align((size_t)n_seq * n_q * 8) + mass_align(attend_workspace_bytes(d, n_seq, n_q, 1));
+}
+
+template <typename T, int D>
+static hipError_t launch_attend_mass_t(const AttendArgs& a, const AttendMass& b, const AttendPlan& p, hipStream_t st) {
+    const dim3 grid((unsigned int)p.ns[0], (unsigned)a.n_seq);
+    const int64_t units = a.n_seq * a.set[0].count;
+    hipError_t e = hipSuccess;
+    if (attend_streams(D * (int)sizeof(T), a)) {
+        if (p.waves == 8) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 8, true, false, true>, grid, dim3(512), 0, st, a);
+        else if constexpr (sizeof(T) == 2) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 4, true, false, true>, grid, dim3(256), 0, st, a);
+    } else if (p.waves == 8) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 8, false, false, true>, grid, dim3(512), 0, st, a);
+    else if constexpr (sizeof(T) == 2) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 4, false, false, true>, grid, dim3(256), 0, st, a);
+    if (e != hipSuccess) return e;
+    const uint64_t merges = p.ns[0] > 1 ? (uint64_t)a.n_seq * a.n_q : 0;
+    const uint64_t all = merges + (uint64_t)a.n_seq * ((a.set[0].count + 4 * kMergeThreads - 1) / (4 * kMergeThreads));
+    if (all >= (uint64_t)1 << 31) return hipErrorInvalidValue;
+    const uint32_t gx = all > 65536 ? 65536u : (uint32_t)all;
+    return launch_timed(kProfAttendMerge, a.n_seq * a.n_q, attend_mass_kernel<T, D>, dim3(gx, (uint32_t)((all + gx - 1) / gx)), dim3(kMergeThreads), 0, st, a, b,
+                        (uint32_t)merges);
+}
+
+hipError_t launch_attend_mass(int dtype, int d, AttendArgs& a, const AttendMass& b, void* workspace, hipStream_t st) {
+    if (a.n_q > 16 || a.set[0].count <= 0 || a.set[1].count != 0) return hipErrorInvalidValue;
+    const AttendPlan p = attend_plan(d, dtype == BKV_BF16 ? 2 : 4, a.n_seq, a.set[0].count, 0, a.n_q, kAttendPartialBytes);
+    a.n_qg = p.n_qg; a.rows = p.rows; a.fused = 0; a.by_xcd = 0;
+    a.ns[0] = p.ns[0]; a.ns[1] = 0; a.set[0].groups_per_split = p.gps[0];
+    char* ws = (char*)workspace;
+    a.logits = (float*)ws;
+    ws += mass_align(logit_bytes(dtype, a.n_seq, a.set[0].count, a.n_q));
+    a.stats = (float*)ws;
+    a.partial = (float*)(ws + mass_align((size_t)a.n_seq * a.n_q * 8));
+    if (dtype == BKV_BF16 && d == 128) return launch_attend_mass_t<__bf16, 128>(a, b, p, st);
+    if (dtype == BKV_BF16 && d == 64) return launch_attend_mass_t<__bf16, 64>(a, b, p, st);
+    if (dtype == BKV_F32 && d == 128) return launch_attend_mass_t<float, 128>(a, b, p, st);
+    if (dtype == BKV_F32 && d == 64) return launch_attend_mass_t<float, 64>(a, b, p, st);
+    return hipErrorInvalidValue;
 }
 
 // Scratch of the entry point that allocates nothing: the split partials live in this array instead of a caller's

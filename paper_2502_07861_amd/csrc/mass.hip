@@ -2,7 +2,10 @@
 //   mass_out_j = decay mass_j + sum_q P_qj,   P_qj = w_j e^{<k_j,q>/sqrt d} / sum_i w_i e^{<k_i,q>/sqrt d}
 // The denominators are known once the attention pass in front of this one is over, so the logits are formed a second time, by
 // keys: a workgroup of four wavefronts keeps 128 keys in registers, 32 each, and its queries go by through LDS, 64 at a time in
-// two buffers.  No weight leaves its lane: lane (n, h) adds up query n's share of its 16 keys, and the 32 lanes meet at the end.
+// two buffers, in the order in which they lie in memory.  No weight leaves its lane: lane (n, h) adds up query n's share of its 16
+// keys, and the 32 lanes meet at the end.
+#include <type_traits>
+
 #include "bkv_device.h"
 #include "bkv_host.h"
 #include "tile_device.h"
@@ -14,31 +17,68 @@ constexpr int kMassKeys = 128;               // keys of a workgroup
 constexpr int kMassRows = 64;                // queries of a tile
 
 template <typename T, int D>
-__global__ __launch_bounds__(kMassThreads) void mass_kernel(const MassArgs a) {
+__global__ __launch_bounds__(kMassThreads, sizeof(T) == 2 ? 3 : 1) void mass_kernel(const MassArgs a) {
     using R = TileRows<T, D>;
-    constexpr int ROWB = R::kRowB, SLOTS = R::kSlots, NP = kMassRows * SLOTS / kMassThreads;
-    __shared__ __align__(16) char lds[2][kMassRows * ROWB];
-    __shared__ __align__(16) floatx2 st[2][kMassRows];
+    using F = TileFetch<T, D>;
+    constexpr int ROWB = R::kRowB, TILEB = kMassRows * ROWB;
+    __shared__ __align__(16) char lds[2][TILEB];
 
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // workgroup -> (sequence, keys, split): the workgroups of a sequence read the same queries and go to one XCD; the first keys of a
+    // causal set, which the most queries see, come first
     const unsigned int block = blockIdx.y * gridDim.x + blockIdx.x;
     const unsigned int per_seq = (unsigned int)a.n_kb * (unsigned int)a.splits;
-    const int64_t seq = block / per_seq;
+    const unsigned int in_xcd = a.by_xcd ? block >> 3 : block;
+    const int64_t seq = a.by_xcd ? (int64_t)(in_xcd / per_seq) * 8 + (block & 7u) : in_xcd / per_seq;
     if (seq >= a.n_seq) return;
-    const int in_seq = (int)(block % per_seq);
-    const int kb = in_seq % a.n_kb, split = in_seq / a.n_kb;
-    const int k0 = kb * kMassKeys + 32 * wave;
-
-    // queries of this workgroup: of a causal set the first ones see none of its keys
-    int r0 = split * a.rows_per_split, r1 = min(a.rows, r0 + a.rows_per_split);
-    if (a.causal) {
-        const int64_t from = (kb * kMassKeys + 1 - a.visible) * a.inner;                // first row that sees the first key
-        if (from > r0) r0 = (int)min(from, (int64_t)r1);
-    }
+    const int in_seq = (int)(in_xcd % per_seq);
+    const int kb = in_seq / a.splits, split = in_seq % a.splits;
+    const int kb0 = kb * kMassKeys, k0 = kb0 + 32 * wave;
 
     const char* Kb = a.K + (size_t)seq * a.stride * ROWB;
+    const char* Qb = a.Q + (size_t)seq * a.rows * ROWB;
+    const floatx2* Sb = reinterpret_cast<const floatx2*>(a.stats) + (size_t)seq * a.rows;
     const float* wb = a.w + (size_t)seq * a.stride;
+
+    // tiles split, split + splits, ... of the sequence's queries (row = head nq + position); of a causal set those of which no query
+    // sees a key are passed over
+    const int tiles = (a.rows + kMassRows - 1) / kMassRows;
+    auto next_tile = [&](int t) {
+        if (a.causal)
+            for (; t < tiles; t += a.splits) {
+                const int first = t * kMassRows, last = min(first + kMassRows, a.rows) - 1;
+                const int most = first / a.nq == last / a.nq ? last % a.nq : a.nq - 1;
+                if (a.visible + most > kb0) break;
+            }
+        return t;
+    };
+    unsigned int qo[F::kSteps];
+#pragma unroll
+    for (int i = 0; i < F::kSteps; ++i) {
+        const int r = 16 * wave + F::row(i, lane);
+        qo[i] = r * ROWB + R::key_slot(r, lane % R::kSlots) * 16;
+    }
+    const unsigned int lds0 = lds_address(&lds[0][0]) + 16 * wave * ROWB;
+    auto fetch = [&](int t, int buf) {
+        const char* from = Qb + (size_t)t * TILEB;
+        const int left = a.rows - 1 - t * kMassRows;
+#pragma unroll
+        for (int i = 0; i < F::kSteps; ++i)                          // (rows past the end repeat it, their statistics say 0)
+            to_lds(from, qo[i] - (left < kMassRows - 1 ? max(16 * wave + F::row(i, lane) - left, 0) * ROWB : 0), lds0 + buf * TILEB + 1024 * i);
+    };
+    floatx2 st0[2], st1[2];
+    auto load_stats = [&](floatx2 (&st)[2], int t) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int r = t * kMassRows + 32 * u + n;
+            st[u] = Sb[min(r, a.rows - 1)];
+            if (r >= a.rows) st[u] = floatx2{-kTileDead, 0.f};
+        }
+    };
+    int t = next_tile(split);
+    if (t < tiles) { fetch(t, 0); load_stats(st0, t); }
+
     uintx4 kf[R::kPieces];
     floatx16 bias;
     {
@@ -47,7 +87,7 @@ __global__ __launch_bounds__(kMassThreads) void mass_kernel(const MassArgs a) {
 #pragma unroll
         for (int c = 0; c < R::kPieces; ++c) {
             kf[c] = *reinterpret_cast<const uintx4*>(Kb + (size_t)key * ROWB + 32 * c + 16 * h);
-            if (!live) kf[c] = uintx4{0u, 0u, 0u, 0u};
+            if (!live) kf[c] = uintx4{0u, 0u, 0u, 0u};               // (whatever the row holds)
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -56,78 +96,62 @@ __global__ __launch_bounds__(kMassThreads) void mass_kernel(const MassArgs a) {
             bias[r] = k < a.count && w > 0.f ? __builtin_amdgcn_logf(w) * a.inv_scale : kTileDead;
         }
     }
-    uintx4 qreg[NP];
-    floatx2 streg = {0.f, 0.f};
-    auto q_row = [&](int r) {
-        const int outer = r / a.inner;
-        return seq * a.q_stream + (int64_t)outer * a.q_outer + (int64_t)(r - outer * a.inner) * a.q_inner;
-    };
-    auto load = [&](int r) {
+    unsigned int ro[R::kPieces];
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int piece = tid + kMassThreads * i;
-            qreg[i] = *reinterpret_cast<const uintx4*>(a.Q + (size_t)q_row(min(r + piece / SLOTS, r1 - 1)) * ROWB + (piece % SLOTS) * 16);
-        }
-        if (tid < kMassRows)
-            streg = r + tid < r1 ? *reinterpret_cast<const floatx2*>(a.stats + 2 * q_row(r + tid)) : floatx2{-kTileDead, 0.f};
-    };
-    auto store = [&](int buf) {
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int piece = tid + kMassThreads * i, r = piece / SLOTS, s = piece % SLOTS;
-            *reinterpret_cast<uintx4*>(lds[buf] + r * ROWB + R::key_slot(r, s) * 16) = qreg[i];
-        }
-        if (tid < kMassRows) st[buf][tid] = streg;
-    };
+    for (int c = 0; c < R::kPieces; ++c) ro[c] = n * ROWB + R::key_slot(n, 2 * c + h) * 16;
     float acc[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[r] = 0.f;
 
-    if (r0 < r1) {
-        load(r0);
-        store(0);
-        __syncthreads();
-        int buf = 0;
-        for (int r = r0;; r += kMassRows) {
-            const bool more = r + kMassRows < r1;
-            if (more) load(r + kMassRows);
+    auto compute = [&](auto buf_c, int tile) {
+        constexpr int BUF = decltype(buf_c)::value;
 #pragma unroll
-            for (int sub = 0; sub < kMassRows / 32; ++sub) {
-                if (r + 32 * sub >= r1) break;
-                const int qr = 32 * sub + n;
-                floatx16 s = bias;
-                if constexpr (R::kB16) {
+        for (int u = 0; u < 2; ++u) {
+            floatx16 s = bias;
+            if constexpr (R::kB16) {
 #pragma unroll
-                    for (int c = 0; c < R::kPieces; ++c)
-                        s = tile_mma<T>(kf[c], *reinterpret_cast<const uintx4*>(lds[buf] + qr * ROWB + R::key_slot(qr, 2 * c + h) * 16), s);
-                } else {
-                    floatx16 s1;
+                for (int c = 0; c < R::kPieces; ++c) s = tile_mma<T>(kf[c], *reinterpret_cast<const uintx4*>(lds[BUF] + ro[c] + 32 * u * ROWB), s);
+            } else {
+                floatx16 s0, s1;
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) s1[x] = 0.f;
-                    floatx16 s0 = s1;
+                for (int x = 0; x < 16; ++x) s0[x] = 0.f;
+                s1 = s0;
 #pragma unroll
-                    for (int c = 0; c < R::kPieces; c += 2) {
-                        s0 = tile_mma<T>(kf[c], *reinterpret_cast<const uintx4*>(lds[buf] + qr * ROWB + R::key_slot(qr, 2 * c + h) * 16), s0);
-                        s1 = tile_mma<T>(kf[c + 1], *reinterpret_cast<const uintx4*>(lds[buf] + qr * ROWB + R::key_slot(qr, 2 * c + 2 + h) * 16), s1);
-                    }
-                    s = s + (s0 + s1);
+                for (int c = 0; c < R::kPieces; c += 2) {
+                    s0 = tile_mma<T>(kf[c], *reinterpret_cast<const uintx4*>(lds[BUF] + ro[c] + 32 * u * ROWB), s0);
+                    s1 = tile_mma<T>(kf[c + 1], *reinterpret_cast<const uintx4*>(lds[BUF] + ro[c + 1] + 32 * u * ROWB), s1);
                 }
-                if (a.causal) {
-                    const int64_t sees = a.visible + min(r + qr, r1 - 1) / a.inner;
-                    if (__builtin_amdgcn_ballot_w64(sees < k0 + 32) != 0ull) {
-#pragma unroll
-                        for (int x = 0; x < 16; ++x) s[x] = k0 + tile_row(x, h) < sees ? s[x] : kTileDead;
-                    }
-                }
-                const floatx2 ml = st[buf][qr];
-#pragma unroll
-                for (int x = 0; x < 16; ++x) acc[x] = fmaf(fast_exp2(fmaf(s[x], a.scale_log2, -ml[0])), ml[1], acc[x]);
+                s = s + (s0 + s1);
             }
-            if (!more) break;
-            store(buf ^ 1);
-            __syncthreads();
-            buf ^= 1;
+            if (a.causal) {
+                const int64_t sees = a.visible + min(tile * kMassRows + 32 * u + n, a.rows - 1) % a.nq;
+                if (__builtin_amdgcn_ballot_w64(sees < k0 + 32) != 0ull) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) s[x] = k0 + tile_row(x, h) < sees ? s[x] : kTileDead;
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < 16; ++x) acc[x] = fmaf(fast_exp2(fmaf(s[x], a.scale_log2, -st0[u][0])), st0[u][1], acc[x]);
         }
+    };
+    if (t < tiles) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0), in the compiler's books too
+        tile_barrier();
+        auto step = [&](auto buf_c) {            // true: this was the last tile
+            constexpr int BUF = decltype(buf_c)::value;
+            const int tn = next_tile(t + a.splits);
+            const bool more = tn < tiles;
+            if (more) { load_stats(st1, tn); fetch(tn, BUF ^ 1); }
+            compute(buf_c, t);
+            if (!more) return true;
+            tile_arrived();
+            tile_barrier();
+            t = tn;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) st0[u] = st1[u];
+            return false;
+        };
+        while (!step(std::integral_constant<int, 0>{}) && !step(std::integral_constant<int, 1>{})) {}
     }
     const int s = lane & 15;
     const float total = xor_sum<16>(row16_transpose_sum(acc, s));
@@ -151,15 +175,16 @@ __global__ __launch_bounds__(kMassThreads) void mass_merge_kernel(const MassArgs
     }
 }
 
-// The queries are split until there are two workgroups per compute unit, so the partial sums are at most so many times its keys.
-constexpr int kMassTarget = 512;
+// The queries are split until there are eight workgroups per compute unit (causal sets: of very different length), so the partial sums are at most so many times its keys.
+constexpr int kMassTarget = 2048;
 size_t mass_part_bytes() { return (size_t)kMassTarget * kMassKeys * sizeof(float); }
 
 static int mass_splits(int64_t n_seq, int64_t count, int64_t rows) {
     const int64_t wgs = n_seq * ((count + kMassKeys - 1) / kMassKeys);
+    // (a workgroup takes the time of two or three tiles to begin and to end: eight tiles each, four where most of the chip is idle)
+    const int64_t most = (rows + kMassRows - 1) / kMassRows / (wgs < 128 ? 4 : 8);
     int64_t splits = kMassTarget / wgs;
-    const int64_t tiles = (rows + kMassRows - 1) / kMassRows;
-    if (splits > tiles) splits = tiles;
+    if (splits > most) splits = most;
     return splits < 1 ? 1 : (int)splits;
 }
 
@@ -167,11 +192,9 @@ template <typename T, int D>
 static hipError_t launch_mass_t(MassArgs& a, hipStream_t st) {
     a.n_kb = (a.count + kMassKeys - 1) / kMassKeys;
     const int splits = mass_splits(a.n_seq, a.count, a.rows);
-    const int tiles = (a.rows + kMassRows - 1) / kMassRows;
-    const int per = (tiles + splits - 1) / splits;
-    a.rows_per_split = per * kMassRows;
-    a.splits = (tiles + per - 1) / per;
-    const uint64_t blocks = (uint64_t)a.n_seq * a.n_kb * a.splits;
+    a.splits = splits;
+    a.by_xcd = a.n_seq >= 8;
+    const uint64_t blocks = (uint64_t)(a.by_xcd ? (a.n_seq + 7) / 8 * 8 : a.n_seq) * a.n_kb * a.splits;
     if (blocks >= (uint64_t)1 << 31) return hipErrorInvalidValue;
     const uint32_t gx = blocks > 65536 ? 65536u : (uint32_t)blocks;
     hipError_t e = launch_timed(kProfAttend, a.n_seq * a.count, mass_kernel<T, D>, dim3(gx, (uint32_t)((blocks + gx - 1) / gx)), dim3(kMassThreads), 0, st, a);
