@@ -290,30 +290,43 @@ def attend_kv_static(p, K_c, V_c, w, Q, out, lse=None, *, count=None):
 
 
 # ------------------------------------------------------------------------------------------ serving: prefix, mass, eviction
-def _here(first, *others):
-    """All tensors on the current device (the stream is this device's), like `first`."""
-    dev = first.device
-    if dev.type != "cuda":
-        raise ValueError("tensors must live on the GPU")
-    if dev.index != torch.cuda.current_device():
-        raise ValueError("tensors live on %s, the current device is cuda:%d" % (dev, torch.cuda.current_device()))
-    for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError("tensors live on %s and on %s" % (dev, t.device))
-
-
-def _shaped(t, shape, what):
-    if t is not None and tuple(t.shape) != tuple(shape):
+def _refuse(t, dtype, shape, dev, what):
+    if dev < 0 or t.get_device() < 0:
+        raise ValueError("%s must live on the GPU" % what)
+    if t.get_device() != dev:
+        raise ValueError("%s lives on cuda:%d, other tensors on cuda:%d" % (what, t.get_device(), dev))
+    if t.dtype != dtype:
+        raise ValueError("%s must be %s, got %s" % (what, dtype, t.dtype))
+    if t.shape != shape:
         raise ValueError("%s must be %s, got %s" % (what, list(shape), list(t.shape)))
+    raise ValueError("%s must be contiguous" % what)
 
 
-def _rows(K, V, w, p, what):
-    """(sequences, places) of a weighted cache after looking at its shapes."""
-    if K.dim() != 3 or K.shape[2] != p.d:
-        raise ValueError("K%s must be [sequences, places, %d], got %s" % (what, p.d, list(K.shape)))
-    _shaped(V, K.shape, "V" + what)
-    _shaped(w, K.shape[:2], "w" + what)
-    return K.shape[0], K.shape[1]
+def _arg(t, dtype, shape, dev, what):
+    """Address of an argument of this type and shape on this device."""
+    if t.dtype != dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _refuse(t, dtype, shape, dev, what)
+    return t.data_ptr()
+
+
+def _device_of(t, what):
+    """Its device, which must be the current one: calls go to the current device's current stream."""
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("%s must live on the GPU" % what)
+    now = torch.cuda.current_device() if _current_device is None else _current_device()
+    if dev != now:
+        raise ValueError("%s lives on cuda:%d, the current device is cuda:%d" % (what, dev, now))
+    return dev
+
+
+def _space(workspace, dev, need):
+    """(address, bytes) of the caller's workspace, or of one for this call, and the tensor that holds it."""
+    if workspace is None:
+        workspace = torch.empty(need(), device=torch.device("cuda", dev), dtype=torch.uint8)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        _refuse(workspace, workspace.dtype, workspace.shape, dev, "workspace")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def attend_prefix_workspace_bytes(p, n_pre, n_seq, g, nq) -> int:
@@ -323,26 +336,28 @@ def attend_prefix_workspace_bytes(p, n_pre, n_seq, g, nq) -> int:
 def attend_prefix(p, prefix, own, Q, *, count_prefix=None, count_own=None, workspace=None, out=None, lse=True):
     """bkv_attend_prefix: prefix = (K, V, w) of n_pre prefixes, own = (K, V, w) of n_seq sequences, sequence s on prefix
     s mod n_pre; Q [n_seq, g, nq, d].  Returns (out, lse or None)."""
-    dt = _torch_dtype(p)
+    dt, f32, d = _torch_dtype(p), torch.float32, p.d
     (Kp, Vp, wp), (Ks, Vs, ws) = prefix, own
-    n_pre, stride_p = _rows(Kp, Vp, wp, p, " of the prefix")
-    n_seq, stride_s = _rows(Ks, Vs, ws, p, " of the sequences")
-    _, g, nq, d = Q.shape
-    _shaped(Q, (n_seq, g, nq, p.d), "Q")
-    _here(Q, Kp, Vp, wp, Ks, Vs, ws, workspace, out)
+    n_pre, stride_p, _ = Kp.shape
+    n_seq, stride_s, _ = Ks.shape
+    _, g, nq, _ = Q.shape
+    dev = _device_of(Q, "Q")
+    rows_p, rows_s, shape = (n_pre, stride_p, d), (n_seq, stride_s, d), (n_seq, g, nq, d)
+    q = _arg(Q, dt, shape, dev, "Q")
     if out is None:
-        out = Q.new_empty((n_seq, g, nq, d), dtype=dt)
-    _shaped(out, Q.shape, "out")
-    lse_t = Q.new_empty((n_seq, g, nq), dtype=torch.float32) if lse else None
-    if workspace is None:
-        workspace = torch.empty(attend_prefix_workspace_bytes(p, n_pre, n_seq, g, nq), device=Q.device, dtype=torch.uint8)
-    f32 = torch.float32
-    rc = lib().bkv_attend_prefix(C.byref(p), _ptr(Kp, dt, "K of the prefix"), _ptr(Vp, dt, "V of the prefix"), _ptr(wp, f32, "w of the prefix"),
-                                 n_pre, stride_p if count_prefix is None else count_prefix, stride_p, _ptr(Ks, dt, "K of the sequences"),
-                                 _ptr(Vs, dt, "V of the sequences"), _ptr(ws, f32, "w of the sequences"), n_seq,
-                                 stride_s if count_own is None else count_own, stride_s, _ptr(Q, dt, "Q"), g, nq, _ptr(out, dt, "out"),
-                                 _ptr(lse_t), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream())
-    _check(rc, "bkv_attend_prefix")
+        out = Q.new_empty(shape)
+        o = out.data_ptr()
+    else:
+        o = _arg(out, dt, shape, dev, "out")
+    lse_t = Q.new_empty((n_seq, g, nq), dtype=f32) if lse else None
+    space, size, _held = _space(workspace, dev, lambda: attend_prefix_workspace_bytes(p, n_pre, n_seq, g, nq))
+    rc = lib().bkv_attend_prefix(C.byref(p), _arg(Kp, dt, rows_p, dev, "K of the prefix"), _arg(Vp, dt, rows_p, dev, "V of the prefix"),
+                                 _arg(wp, f32, rows_p[:2], dev, "w of the prefix"), n_pre, stride_p if count_prefix is None else count_prefix,
+                                 stride_p, _arg(Ks, dt, rows_s, dev, "K of the sequences"), _arg(Vs, dt, rows_s, dev, "V of the sequences"),
+                                 _arg(ws, f32, rows_s[:2], dev, "w of the sequences"), n_seq, stride_s if count_own is None else count_own,
+                                 stride_s, q, g, nq, o, None if lse_t is None else lse_t.data_ptr(), space, size, _stream())
+    if rc < 0:
+        raise BkvError(rc, "bkv_attend_prefix")
     return out, lse_t
 
 
@@ -354,31 +369,31 @@ def attend_mass(p, K_c, V_c, w, Q, mass=None, *, count=None, visible=None, decay
     """bkv_attend_mass: attend_kv, and the tokens' accumulated attention weight.  K_c, V_c [n_seq, stride, d]; w, mass
     [n_seq, stride] (mass None: zeros); Q [n_seq, g, nq, d]; query i sees the first visible + i places (None: all).  mass_out
     may be mass.  Returns (out, lse or None, mass_out); a new mass_out is 0 from `count` on."""
-    dt = _torch_dtype(p)
-    n_seq, stride = _rows(K_c, V_c, w, p, "_c")
-    _, g, nq, d = Q.shape
-    _shaped(Q, (n_seq, g, nq, p.d), "Q")
-    _shaped(mass, (n_seq, stride), "mass")
-    _shaped(mass_out, (n_seq, stride), "mass_out")
-    _here(Q, K_c, V_c, w, mass, mass_out, workspace, out)
+    dt, f32, d = _torch_dtype(p), torch.float32, p.d
+    n_seq, stride, _ = K_c.shape
+    _, g, nq, _ = Q.shape
+    dev = _device_of(Q, "Q")
+    rows, per, shape = (n_seq, stride, d), (n_seq, stride), (n_seq, g, nq, d)
+    q = _arg(Q, dt, shape, dev, "Q")
+    k, v, at_w = _arg(K_c, dt, rows, dev, "K_c"), _arg(V_c, dt, rows, dev, "V_c"), _arg(w, f32, per, dev, "w")
+    m = None if mass is None else _arg(mass, f32, per, dev, "mass")
     if count is None:
         count = stride
     if visible is None:
         visible = count
     if out is None:
-        out = Q.new_empty((n_seq, g, nq, d), dtype=dt)
-    _shaped(out, Q.shape, "out")
-    lse_t = Q.new_empty((n_seq, g, nq), dtype=torch.float32) if lse else None
+        out = Q.new_empty(shape)
+        o = out.data_ptr()
+    else:
+        o = _arg(out, dt, shape, dev, "out")
+    lse_t = Q.new_empty((n_seq, g, nq), dtype=f32) if lse else None
     if mass_out is None:
-        mass_out = w.new_empty((n_seq, stride)) if count == stride else w.new_zeros((n_seq, stride))
-    if workspace is None:
-        workspace = torch.empty(attend_mass_workspace_bytes(p, n_seq, count, g, nq), device=Q.device, dtype=torch.uint8)
-    f32 = torch.float32
-    rc = lib().bkv_attend_mass(C.byref(p), _ptr(K_c, dt, "K_c"), _ptr(V_c, dt, "V_c"), _ptr(w, f32, "w"), n_seq, count, stride, _ptr(Q, dt, "Q"),
-                               g, nq, max(min(visible, 1 << 40), -(1 << 40)), float(decay), _ptr(mass, f32, "mass"), _ptr(out, dt, "out"),
-                               _ptr(lse_t), _ptr(mass_out, f32, "mass_out"), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                               _stream())
-    _check(rc, "bkv_attend_mass")
+        mass_out = w.new_empty(per) if count == stride else w.new_zeros(per)
+    space, size, _held = _space(workspace, dev, lambda: attend_mass_workspace_bytes(p, n_seq, count, g, nq))
+    rc = lib().bkv_attend_mass(C.byref(p), k, v, at_w, n_seq, count, stride, q, g, nq, max(min(visible, 1 << 40), -(1 << 40)), decay, m, o,
+                               None if lse_t is None else lse_t.data_ptr(), _arg(mass_out, f32, per, dev, "mass_out"), space, size, _stream())
+    if rc < 0:
+        raise BkvError(rc, "bkv_attend_mass")
     return out, lse_t, mass_out
 
 
@@ -386,29 +401,34 @@ def evict_workspace_bytes(p, n_seq, count) -> int:
     return int(lib().bkv_evict_workspace_bytes(C.byref(p), n_seq, count))
 
 
-def evict(p, K_c, V_c, w, mass, keep, *, n_sink=0, n_recent=0, count=None, idx=None, workspace=None):
+def evict(p, K_c, V_c, w, mass, keep, *, n_sink=0, n_recent=0, count=None, idx=None, workspace=None, out=None):
     """bkv_evict: the heaviest `keep` tokens of every sequence by mass [n_seq, stride], the first n_sink and the last n_recent
-    among them.  Returns dict(K, V, w, mass, idx [n_seq, keep], count [n_seq])."""
-    dt = _torch_dtype(p)
-    n_seq, stride = _rows(K_c, V_c, w, p, "_c")
-    _shaped(mass, (n_seq, stride), "mass")
-    _shaped(idx, (n_seq, stride), "idx")
-    _here(K_c, V_c, w, mass, idx, workspace)
+    among them.  Returns dict(K, V, w, mass, idx [n_seq, keep], count [n_seq]), `out` if it is given."""
+    dt, f32, d = _torch_dtype(p), torch.float32, p.d
+    n_seq, stride, _ = K_c.shape
+    dev = _device_of(K_c, "K_c")
+    rows, per = (n_seq, stride, d), (n_seq, stride)
+    k, v, at_w, m = _arg(K_c, dt, rows, dev, "K_c"), _arg(V_c, dt, rows, dev, "V_c"), _arg(w, f32, per, dev, "w"), _arg(mass, f32, per, dev, "mass")
+    i = None if idx is None else _arg(idx, torch.int32, per, dev, "idx")
     if count is None:
         count = stride
     if not 0 <= keep <= count <= stride:
         raise ValueError("keep %d of %d places, %d stored" % (keep, count, stride))
-    new, f32 = K_c.new_empty, torch.float32
-    res = dict(K=new((n_seq, keep, p.d), dtype=dt), V=new((n_seq, keep, p.d), dtype=dt), w=new((n_seq, keep), dtype=f32),
-               mass=new((n_seq, keep), dtype=f32), idx=new((n_seq, keep), dtype=torch.int32), count=new((n_seq,), dtype=torch.int32))
-    if workspace is None:
-        workspace = torch.empty(evict_workspace_bytes(p, n_seq, count), device=K_c.device, dtype=torch.uint8)
-    rc = lib().bkv_evict(C.byref(p), _ptr(K_c, dt, "K_c"), _ptr(V_c, dt, "V_c"), _ptr(w, f32, "w"), _ptr(mass, f32, "mass"),
-                         _ptr(idx, torch.int32, "idx"), n_seq, count, stride, keep, n_sink, n_recent, _ptr(res["K"]), _ptr(res["V"]),
-                         _ptr(res["w"]), _ptr(res["mass"]), _ptr(res["idx"]), _ptr(res["count"]), _ptr(workspace),
-                         workspace.numel() * workspace.element_size(), _stream())
-    _check(rc, "bkv_evict")
-    return res
+    rows, per = (n_seq, keep, d), (n_seq, keep)
+    if out is None:
+        new = K_c.new_empty
+        out = dict(K=new(rows), V=new(rows), w=new(per, dtype=f32), mass=new(per, dtype=f32), idx=new(per, dtype=torch.int32),
+                   count=new((n_seq,), dtype=torch.int32))
+        res = [t.data_ptr() for t in out.values()]
+    else:
+        res = [_arg(out["K"], dt, rows, dev, "out K"), _arg(out["V"], dt, rows, dev, "out V"), _arg(out["w"], f32, per, dev, "out w"),
+               _arg(out["mass"], f32, per, dev, "out mass"), _arg(out["idx"], torch.int32, per, dev, "out idx"),
+               _arg(out["count"], torch.int32, (n_seq,), dev, "out count")]
+    space, size, _held = _space(workspace, dev, lambda: evict_workspace_bytes(p, n_seq, count))
+    rc = lib().bkv_evict(C.byref(p), k, v, at_w, m, i, n_seq, count, stride, keep, n_sink, n_recent, *res, space, size, _stream())
+    if rc < 0:
+        raise BkvError(rc, "bkv_evict")
+    return out
 
 
 # ------------------------------------------------------------------------------------------ Alg. 1: buckets, two instances
