@@ -482,7 +482,11 @@ int bkv_attend_prefix(const bkv_params* p, const void* K_p, const void* V_p, con
     int jobs = 0;
     if (count_p > 0) a.job[jobs++] = pre;
     if (count_s > 0) a.job[jobs++] = own;
-    for (int k = 0; k < jobs; ++k) bkv::tile_plan(a.job[k]);
+    int64_t taken = 0;
+    for (int k = jobs - 1; k >= 0; --k) {                  // (the own tokens first: the prefix is cut into what they leave room for)
+        bkv::tile_plan(a.job[k], taken);
+        taken += (int64_t)a.job[k].n_streams * a.job[k].n_qt * a.job[k].splits;
+    }
     const hipError_t e = bkv::launch_tiles(p->dtype, p->d, a, jobs, (float*)workspace, st);
     return e == hipSuccess ? BKV_OK : hip_fail(e);
 }
@@ -539,7 +543,7 @@ int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const
     char* ws = (char*)workspace;
     a.stats = (float*)ws;
     ws += align_up((size_t)n_seq * n_q * 8, 256);
-    bkv::tile_plan(j);
+    bkv::tile_plan(j, 0);
     hipError_t e = bkv::launch_tiles(p->dtype, p->d, a, 1, (float*)ws, st);
     if (e != hipSuccess) return hip_fail(e);
     const int splits = bkv::tile_most_splits(n_seq, n_q);

@@ -41,15 +41,25 @@ __global__ __launch_bounds__(kMassThreads, sizeof(T) == 2 ? 3 : 1) void mass_ker
     const floatx2* Sb = reinterpret_cast<const floatx2*>(a.stats) + (size_t)seq * a.rows;
     const float* wb = a.w + (size_t)seq * a.stride;
 
+    // keys of this wavefront, on their way first
+    uintx4 kf[R::kPieces];
+    const int key = min(k0 + n, a.count - 1);
+#pragma unroll
+    for (int c = 0; c < R::kPieces; ++c) kf[c] = *reinterpret_cast<const uintx4*>(Kb + (size_t)key * ROWB + 32 * c + 16 * h);
+    const float w_raw = wb[key], w = k0 + n < a.count ? w_raw : 0.f;
+
     // tiles split, split + splits, ... of the sequence's queries (row = head nq + position); of a causal set those of which no query
-    // sees a key are passed over
+    // sees a key are passed over.  p0: position of the tile's first row
     const int tiles = (a.rows + kMassRows - 1) / kMassRows;
+    int p0 = a.causal ? split * kMassRows % a.nq : 0;
+    const int p_step = a.causal ? a.splits * kMassRows % a.nq : 0;
+    auto in_one_head = [&](int t) { return p0 + min(kMassRows, a.rows - t * kMassRows) <= a.nq; };
     auto next_tile = [&](int t) {
         if (a.causal)
             for (; t < tiles; t += a.splits) {
-                const int first = t * kMassRows, last = min(first + kMassRows, a.rows) - 1;
-                const int most = first / a.nq == last / a.nq ? last % a.nq : a.nq - 1;
-                if (a.visible + most > kb0) break;
+                if (a.visible + (in_one_head(t) ? p0 + min(kMassRows, a.rows - t * kMassRows) - 1 : a.nq - 1) > kb0) break;
+                p0 += p_step;
+                if (p0 >= a.nq) p0 -= a.nq;
             }
         return t;
     };
@@ -79,22 +89,17 @@ __global__ __launch_bounds__(kMassThreads, sizeof(T) == 2 ? 3 : 1) void mass_ker
     int t = next_tile(split);
     if (t < tiles) { fetch(t, 0); load_stats(st0, t); }
 
-    uintx4 kf[R::kPieces];
-    floatx16 bias;
+    floatx16 bias;                               // log2 w of the keys, in units of 1 / scale
     {
-        const int key = min(k0 + n, a.count - 1);
-        const bool live = k0 + n < a.count && wb[key] > 0.f;
+        const bool live = w > 0.f;
+        if (__ballot(!live) != 0ull) {
 #pragma unroll
-        for (int c = 0; c < R::kPieces; ++c) {
-            kf[c] = *reinterpret_cast<const uintx4*>(Kb + (size_t)key * ROWB + 32 * c + 16 * h);
-            if (!live) kf[c] = uintx4{0u, 0u, 0u, 0u};               // (whatever the row holds)
+            for (int c = 0; c < R::kPieces; ++c)
+                if (!live) kf[c] = uintx4{0u, 0u, 0u, 0u};           // (whatever the row holds)
         }
+        const float mine = live ? __builtin_amdgcn_logf(w) * a.inv_scale : kTileDead;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int k = k0 + tile_row(r, h);
-            const float w = wb[min(k, a.count - 1)];
-            bias[r] = k < a.count && w > 0.f ? __builtin_amdgcn_logf(w) * a.inv_scale : kTileDead;
-        }
+        for (int r = 0; r < 16; ++r) bias[r] = __shfl(mine, tile_row(r, h));
     }
     unsigned int ro[R::kPieces];
 #pragma unroll
@@ -105,6 +110,7 @@ __global__ __launch_bounds__(kMassThreads, sizeof(T) == 2 ? 3 : 1) void mass_ker
 
     auto compute = [&](auto buf_c, int tile) {
         constexpr int BUF = decltype(buf_c)::value;
+        const bool masked = a.causal && a.visible + (in_one_head(tile) ? p0 : 0) < k0 + 32;        // a query does not see all keys
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             floatx16 s = bias;
@@ -123,12 +129,11 @@ __global__ __launch_bounds__(kMassThreads, sizeof(T) == 2 ? 3 : 1) void mass_ker
                 }
                 s = s + (s0 + s1);
             }
-            if (a.causal) {
-                const int64_t sees = a.visible + min(tile * kMassRows + 32 * u + n, a.rows - 1) % a.nq;
-                if (__builtin_amdgcn_ballot_w64(sees < k0 + 32) != 0ull) {
+            if (masked) {
+                const int r = min(tile * kMassRows + 32 * u + n, a.rows - 1) - tile * kMassRows;
+                const int64_t sees = a.visible + (p0 + r) % a.nq;
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) s[x] = k0 + tile_row(x, h) < sees ? s[x] : kTileDead;
-                }
+                for (int x = 0; x < 16; ++x) s[x] = k0 + tile_row(x, h) < sees ? s[x] : kTileDead;
             }
 #pragma unroll
             for (int x = 0; x < 16; ++x) acc[x] = fmaf(fast_exp2(fmaf(s[x], a.scale_log2, -st0[u][0])), st0[u][1], acc[x]);
@@ -139,11 +144,16 @@ __global__ __launch_bounds__(kMassThreads, sizeof(T) == 2 ? 3 : 1) void mass_ker
         tile_barrier();
         auto step = [&](auto buf_c) {            // true: this was the last tile
             constexpr int BUF = decltype(buf_c)::value;
-            const int tn = next_tile(t + a.splits);
+            const int p_now = p0;
+            p0 += p_step;
+            if (p0 >= a.nq) p0 -= a.nq;
+            const int tn = next_tile(t + a.splits), p_next = p0;
             const bool more = tn < tiles;
             if (more) { load_stats(st1, tn); fetch(tn, BUF ^ 1); }
+            p0 = p_now;
             compute(buf_c, t);
             if (!more) return true;
+            p0 = p_next;
             tile_arrived();
             tile_barrier();
             t = tn;
@@ -155,12 +165,12 @@ __global__ __launch_bounds__(kMassThreads, sizeof(T) == 2 ? 3 : 1) void mass_ker
     }
     const int s = lane & 15;
     const float total = xor_sum<16>(row16_transpose_sum(acc, s));
-    const int key = k0 + tile_row(s, h);
-    if ((lane & 16) != 0 || key >= a.count) return;
+    const int to = k0 + tile_row(s, h);
+    if ((lane & 16) != 0 || to >= a.count) return;
     if (a.splits > 1) {
-        a.part[((size_t)split * a.n_seq + seq) * a.count + key] = total;
+        a.part[((size_t)split * a.n_seq + seq) * a.count + to] = total;
     } else {
-        const size_t at = (size_t)seq * a.stride + key;
+        const size_t at = (size_t)seq * a.stride + to;
         a.mass_out[at] = a.mass ? fmaf(a.decay, a.mass[at], total) : total;
     }
 }

@@ -145,6 +145,7 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
         const char* Vt = lds.rows[BUF][1];
         const int k0 = t * kTileKeys + (NS == 1 ? 32 * ksub : 0);
         // ---- logits, in units of 1 / scale
+        __builtin_amdgcn_s_setprio(1);
         floatx16 s[NS];
 #pragma unroll
         for (int u = 0; u < NS; ++u) {
@@ -165,6 +166,7 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
                 s[u] = s[u] + s1;
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         // ---- token weights: one for the whole tile (the usual tile), or ln2 w of every key as one more product: its three bf16
         // parts (together all its bits) times ones, in the half of the wavefront that holds the group's keys
         const float first = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(w)));
@@ -453,12 +455,19 @@ int tile_most_splits(int64_t n_streams, int64_t rows) {
     return wgs > 0 ? (int)max((int64_t)1, kTileTarget / wgs) : 1;
 }
 
-void tile_plan(TileJob& j) {
+// taken: workgroups of the launch that others have
+void tile_plan(TileJob& j, int64_t taken) {
     j.qw = tile_qw(j.rows);
     j.n_qt = (j.rows + 32 * j.qw - 1) / (32 * j.qw);
     const int tiles = (j.count + kTileKeys - 1) / kTileKeys;
     int splits = tile_most_splits(j.n_streams, j.rows);
-    if (splits > tiles) splits = tiles;
+    // (A few others that the chip has no place for beside these cost a second round: 512 + 32 workgroups, two a compute unit, 11.6 us,
+    // 256 + 32 of them with twice the keys 7.7.  Many others are the launch's work themselves.)
+    const int64_t room = (kTileTarget - (taken <= kTileTarget / 8 ? taken : 0)) / ((int64_t)j.n_streams * j.n_qt);
+    if (splits > room) splits = (int)room;
+    // (a split of full workgroups writes 128 rows of sums: eight tiles of keys at least)
+    const int most = j.qw == 4 ? (tiles + 7) / 8 : tiles;
+    if (splits > most) splits = most;
     if (splits < 1) splits = 1;
     j.tiles_per_split = (tiles + splits - 1) / splits;
     j.splits = j.tiles_per_split > 0 ? (tiles + j.tiles_per_split - 1) / j.tiles_per_split : 1;
