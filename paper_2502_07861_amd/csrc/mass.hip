@@ -178,8 +178,15 @@ __global__ __launch_bounds__(kMassThreads, sizeof(T) == 2 ? 3 : 1) void mass_ker
 __global__ __launch_bounds__(kMassThreads) void mass_merge_kernel(const MassArgs a) {
     const int64_t seq = blockIdx.y;
     for (int64_t key = (int64_t)blockIdx.x * kMassThreads + threadIdx.x; key < a.count; key += (int64_t)gridDim.x * kMassThreads) {
+        constexpr int U = 8;                                         // partial sums on their way at a time
         float total = 0.f;
-        for (int s = 0; s < a.splits; ++s) total += a.part[((size_t)s * a.n_seq + seq) * a.count + key];
+        for (int s0 = 0; s0 < a.splits; s0 += U) {
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = a.part[((size_t)min(s0 + u, a.splits - 1) * a.n_seq + seq) * a.count + key];
+#pragma unroll
+            for (int u = 0; u < U; ++u) total += s0 + u < a.splits ? x[u] : 0.f;
+        }
         const size_t at = (size_t)seq * a.stride + key;
         a.mass_out[at] = a.mass ? fmaf(a.decay, a.mass[at], total) : total;
     }
@@ -189,11 +196,14 @@ __global__ __launch_bounds__(kMassThreads) void mass_merge_kernel(const MassArgs
 constexpr int kMassTarget = 2048;
 size_t mass_part_bytes() { return (size_t)kMassTarget * kMassKeys * sizeof(float); }
 
-static int mass_splits(int64_t n_seq, int64_t count, int64_t rows) {
+static int mass_splits(int64_t n_seq, int64_t count, int64_t rows, int elem) {
     const int64_t wgs = n_seq * ((count + kMassKeys - 1) / kMassKeys);
-    // (a workgroup takes the time of two or three tiles to begin and to end: eight tiles each, four where most of the chip is idle)
-    const int64_t most = (rows + kMassRows - 1) / kMassRows / (wgs < 128 ? 4 : 8);
-    int64_t splits = kMassTarget / wgs;
+    // (bf16: a workgroup takes the time of two or three tiles to begin and to end: eight tiles each, where there are workgroups enough.
+    // fp32: a tile takes longer than that by itself.)
+    const int64_t tiles = (rows + kMassRows - 1) / kMassRows, fill = (256 + wgs - 1) / wgs;
+    int64_t most = elem == 2 ? tiles / 8 > fill ? tiles / 8 : fill : tiles;
+    if (most > tiles) most = tiles;
+    int64_t splits = (elem == 2 ? kMassTarget : kMassTarget / 2) / wgs;
     if (splits > most) splits = most;
     return splits < 1 ? 1 : (int)splits;
 }
@@ -201,9 +211,9 @@ static int mass_splits(int64_t n_seq, int64_t count, int64_t rows) {
 template <typename T, int D>
 static hipError_t launch_mass_t(MassArgs& a, hipStream_t st) {
     a.n_kb = (a.count + kMassKeys - 1) / kMassKeys;
-    const int splits = mass_splits(a.n_seq, a.count, a.rows);
+    const int splits = mass_splits(a.n_seq, a.count, a.rows, (int)sizeof(T));
     a.splits = splits;
-    a.by_xcd = a.n_seq >= 8;
+    a.by_xcd = a.n_seq % 8 == 0 || a.n_seq >= 48;              // (equal shares for all XCDs)
     const uint64_t blocks = (uint64_t)(a.by_xcd ? (a.n_seq + 7) / 8 * 8 : a.n_seq) * a.n_kb * a.splits;
     if (blocks >= (uint64_t)1 << 31) return hipErrorInvalidValue;
     const uint32_t gx = blocks > 65536 ? 65536u : (uint32_t)blocks;

@@ -366,10 +366,11 @@ __global__ __launch_bounds__(kTileThreads, sizeof(T) == 2 ? 2 : 1) void tile_ker
     const int which = block >= a.first ? 1 : 0;
     block -= which ? a.first : 0u;
     const TileJob J = which ? a.job[1] : a.job[0];
-    const unsigned int in_xcd = block >> 3;
-    const unsigned int unit = in_xcd / (unsigned int)J.n_qt * 8u + (block & 7u);
-    const int qt = J.n_qt - 1 - (int)(in_xcd % (unsigned int)J.n_qt);           // (causal: the longest first)
-    if (unit >= (unsigned int)J.n_streams * (unsigned int)J.splits) return;
+    const unsigned int units = (unsigned int)J.n_streams * (unsigned int)J.splits, in_xcd = block >> 3;
+    const unsigned int unit = J.by_xcd ? in_xcd / (unsigned int)J.n_qt * 8u + (block & 7u) : block % units;
+    const unsigned int turn = J.by_xcd ? in_xcd % (unsigned int)J.n_qt : block / units;
+    if (unit >= units || turn >= (unsigned int)J.n_qt) return;
+    const int qt = J.n_qt - 1 - (int)turn;                                      // (causal: the longest first)
     const int split = (int)(unit % (unsigned int)J.splits);
     const int64_t stream = unit / (unsigned int)J.splits;
     if (J.qw == 4) tile_body<T, D, 4>(a, J, stream, split, qt, lds);
@@ -446,31 +447,38 @@ __global__ __launch_bounds__(kTileMergeThreads) void tile_merge_kernel(const Til
 
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kTileTarget = 512;             // workgroups a launch is cut into where there are fewer: two per compute unit
+constexpr int kTileFull = 256;               // ... one
 
 static int tile_qw(int64_t rows) { return rows > 64 ? 4 : rows > 32 ? 2 : 1; }
+static int64_t tile_units(int64_t n_streams, int64_t rows, int qw) { return n_streams * ((rows + 32 * qw - 1) / (32 * qw)); }
 
-// Splits of a job of this shape at most (any token count).
+// Splits of a job of this shape at most (any token count; with fewer queries to a workgroup there are more workgroups, and fewer splits).
 int tile_most_splits(int64_t n_streams, int64_t rows) {
-    const int64_t wgs = n_streams * ((rows + 32 * tile_qw(rows) - 1) / (32 * tile_qw(rows)));
+    const int64_t wgs = tile_units(n_streams, rows, tile_qw(rows));
     return wgs > 0 ? (int)max((int64_t)1, kTileTarget / wgs) : 1;
 }
 
-// taken: workgroups of the launch that others have
-void tile_plan(TileJob& j, int64_t taken) {
-    j.qw = tile_qw(j.rows);
-    j.n_qt = (j.rows + 32 * j.qw - 1) / (32 * j.qw);
+// Queries of a workgroup and cuts of the keys.  Workgroups of 128 queries read the fewest keys; where they do not give every compute
+// unit one even with the keys cut, smaller ones are taken.  A cut of a workgroup of 128 queries costs 128 rows of sums written and
+// read, on bf16 about what two tiles of 64 keys take, so it gets eight of those where there are workgroups enough (in fp32 a tile takes
+// four times as long and no minimum is kept).  taken: workgroups of the launch that others have.
+void tile_plan(TileJob& j, int elem, int64_t taken) {
     const int tiles = (j.count + kTileKeys - 1) / kTileKeys;
-    int splits = tile_most_splits(j.n_streams, j.rows);
-    // (A few others that the chip has no place for beside these cost a second round: 512 + 32 workgroups, two a compute unit, 11.6 us,
-    // 256 + 32 of them with twice the keys 7.7.  Many others are the launch's work themselves.)
-    const int64_t room = (kTileTarget - (taken <= kTileTarget / 8 ? taken : 0)) / ((int64_t)j.n_streams * j.n_qt);
-    if (splits > room) splits = (int)room;
-    // (a split of full workgroups writes 128 rows of sums: eight tiles of keys at least)
-    const int most = j.qw == 4 ? (tiles + 7) / 8 : tiles;
-    if (splits > most) splits = most;
-    if (splits < 1) splits = 1;
-    j.tiles_per_split = (tiles + splits - 1) / splits;
-    j.splits = j.tiles_per_split > 0 ? (tiles + j.tiles_per_split - 1) / j.tiles_per_split : 1;
+    for (j.qw = tile_qw(j.rows);; j.qw /= 2) {
+        const int64_t wgs = tile_units(j.n_streams, j.rows, j.qw);
+        j.n_qt = (j.rows + 32 * j.qw - 1) / (32 * j.qw);
+        // (A few others that the chip has no place for beside these cost a second round: 512 + 32 workgroups, two a compute unit, 11.6 us,
+        // 256 + 32 of them with twice the keys 7.7.  Many others are the launch's work themselves.)
+        int64_t splits = (kTileTarget - (taken <= kTileTarget / 8 ? taken : 0)) / wgs;
+        if (j.qw == 4 && elem == 2) splits = min(splits, max((int64_t)(tiles + 7) / 8, (kTileFull + wgs - 1) / wgs));
+        splits = max((int64_t)1, min(splits, (int64_t)tiles));
+        j.tiles_per_split = (int)((tiles + splits - 1) / splits);
+        j.splits = j.tiles_per_split > 0 ? (tiles + j.tiles_per_split - 1) / j.tiles_per_split : 1;
+        if (j.qw == 1 || wgs * j.splits >= kTileFull * 3 / 4) break;
+    }
+    // XCDs take the query tiles of a split each where that gives them equal shares, else whatever comes next
+    const int64_t units = (int64_t)j.n_streams * j.splits;
+    j.by_xcd = units % 8 == 0 || units >= 48;
 }
 
 size_t tile_part_bytes(int d, int64_t n_rows, int splits) { return (size_t)n_rows * splits * (d + kTilePad) * sizeof(float); }
@@ -482,7 +490,8 @@ static hipError_t launch_tiles_t(TileArgs& a, int n_jobs, float* part, hipStream
     for (int k = 0; k < n_jobs; ++k) {
         TileJob& j = a.job[k];
         if (k == 1) a.first = (uint32_t)blocks;
-        blocks += ((uint64_t)j.n_streams * j.splits + 7) / 8 * 8 * j.n_qt;
+        const uint64_t own = (uint64_t)j.n_streams * j.splits;
+        blocks += j.by_xcd ? (own + 7) / 8 * 8 * j.n_qt : (own * j.n_qt + 7) / 8 * 8;
         units += (uint64_t)j.n_streams * j.count;
         splits += j.splits;
     }
