@@ -451,7 +451,7 @@ extern "C" {
 
 size_t bkv_attend_prefix_workspace_bytes(const bkv_params* p, int64_t n_pre, int64_t n_seq, int32_t g, int32_t nq) {
     if (check_queries(p, n_seq, g, nq) || n_pre <= 0 || n_seq % n_pre) return 0;
-    const int splits = bkv::tile_most_splits(n_pre, n_seq / n_pre * g * nq) + bkv::tile_most_splits(n_seq, (int64_t)g * nq);
+    const int splits = bkv::tile_most_splits(n_pre, n_seq / n_pre * g * nq, elem_bytes(p), false) + bkv::tile_most_splits(n_seq, (int64_t)g * nq, elem_bytes(p), false);
     return align_up(bkv::tile_part_bytes(p->d, n_seq * g * nq, splits), 256);
 }
 
@@ -484,7 +484,7 @@ int bkv_attend_prefix(const bkv_params* p, const void* K_p, const void* V_p, con
     if (count_s > 0) a.job[jobs++] = own;
     int64_t taken = 0;
     for (int k = jobs - 1; k >= 0; --k) {                  // (the own tokens first: the prefix is cut into what they leave room for)
-        bkv::tile_plan(a.job[k], elem_bytes(p), taken);
+        bkv::tile_plan(a.job[k], elem_bytes(p), false, taken);
         taken += (int64_t)a.job[k].n_streams * a.job[k].n_qt * a.job[k].splits;
     }
     const hipError_t e = bkv::launch_tiles(p->dtype, p->d, a, jobs, (float*)workspace, st);
@@ -494,7 +494,7 @@ int bkv_attend_prefix(const bkv_params* p, const void* K_p, const void* V_p, con
 size_t bkv_attend_mass_workspace_bytes(const bkv_params* p, int64_t n_seq, int64_t count, int32_t g, int32_t nq) {
     if (check_queries(p, n_seq, g, nq) || count < 0) return 0;
     const int64_t n_q = (int64_t)g * nq;
-    const int splits = bkv::tile_most_splits(n_seq, n_q);
+    const int splits = bkv::tile_most_splits(n_seq, n_q, elem_bytes(p), true);
     const size_t tiles = align_up((size_t)n_seq * n_q * 8, 256) + (splits > 1 ? align_up(bkv::tile_part_bytes(p->d, n_seq * n_q, splits), 256) : 0) +
                          bkv::mass_part_bytes();
     if (!bkv::attend_keeps_logits(row_bytes(p), n_q)) return tiles;
@@ -543,10 +543,10 @@ int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const
     char* ws = (char*)workspace;
     a.stats = (float*)ws;
     ws += align_up((size_t)n_seq * n_q * 8, 256);
-    bkv::tile_plan(j, elem_bytes(p), 0);
+    bkv::tile_plan(j, elem_bytes(p), a.causal, 0);
     hipError_t e = bkv::launch_tiles(p->dtype, p->d, a, 1, (float*)ws, st);
     if (e != hipSuccess) return hip_fail(e);
-    const int splits = bkv::tile_most_splits(n_seq, n_q);
+    const int splits = bkv::tile_most_splits(n_seq, n_q, elem_bytes(p), true);
     if (splits > 1) ws += align_up(bkv::tile_part_bytes(p->d, n_seq * n_q, splits), 256);
     bkv::MassArgs b;
     memset(&b, 0, sizeof(b));

@@ -18,8 +18,11 @@ constexpr int kTileKeys = 64;
 constexpr int kTileThreads = 256;
 constexpr int kTilePad = 4;                  // floats behind the D sums of a partial row: [0] reference exponent, [1] denominator
 
+// Two tiles, so that the next one is on its way while one is multiplied; of rows of 512 bytes (fp32, whose products take four times as
+// long as their loads) one, and two workgroups a compute unit that wait in turn.
 template <typename T, int D> struct TileLds {
-    __align__(16) char rows[2][2][kTileKeys * D * sizeof(T)];        // [buffer][keys, values]
+    static constexpr int kBuffers = D * sizeof(T) == 512 ? 1 : 2;
+    __align__(16) char rows[kBuffers][2][kTileKeys * D * sizeof(T)];        // [buffer][keys, values]
 };
 
 // QW: wavefronts with queries of their own; 4 / QW share the same ones.
@@ -28,7 +31,9 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
     using R = TileRows<T, D>;
     using F = TileFetch<T, D>;
     constexpr int ROWB = R::kRowB, EPN = R::kEpn, P = D + kTilePad, TILEB = kTileKeys * ROWB;
-    constexpr int KW = 4 / QW, NS = QW == 4 ? 2 : 1;                 // wavefronts a query has; groups of 32 keys a wavefront takes of a tile
+    constexpr int BUFS = TileLds<T, D>::kBuffers;
+    // wavefronts a query has; groups of 32 keys a wavefront takes of a tile at a time, times (fp32: registers)
+    constexpr int KW = 4 / QW, NS = QW == 4 && R::kB16 ? 2 : 1, TIMES = QW == 4 ? 2 / NS : 1;
     // bf16: a weight multiplies its value row as two bf16 numbers, its upper bits and what they leave (relative error 2^-17), except
     // for full workgroups of 128 queries, where the matrix cores are the bound: there it is rounded to one (2^-8), as the result is.
     // 8 prefixes x 16385 tokens x 1280 queries: 165 -> 137 us, off the 64-bit result 1.7e-3 -> 2.1e-3 (rounding it makes 1.7e-3).
@@ -111,15 +116,15 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
     // where a lane reads: key row n (of the wavefront's group), value columns (see tile_device.h)
     unsigned int ko[R::kPieces];
 #pragma unroll
-    for (int c = 0; c < R::kPieces; ++c) ko[c] = (NS == 1 ? ksub * 32 * ROWB : 0) + n * ROWB + R::key_slot(n, 2 * c + h) * 16;
+    for (int c = 0; c < R::kPieces; ++c) ko[c] = ksub * 32 * ROWB + n * ROWB + R::key_slot(n, 2 * c + h) * 16;
     constexpr int NV = R::kB16 ? EPN : 1;
     unsigned int vo[NV];
     if constexpr (R::kB16) {
         const int i16 = lane & 15, half = (lane >> 4) & 1, r = 4 * h + (i16 >> 2);
 #pragma unroll
         for (int e = 0; e < EPN; ++e)
-            vo[e] = (NS == 1 ? ksub * 32 * ROWB : 0) + r * ROWB + R::value_slot(r, 4 * e + 2 * half + ((i16 & 3) >> 1)) * 16 + (i16 & 1) * 8;
-    } else vo[0] = (NS == 1 ? ksub * 32 * ROWB : 0) + 4 * h * ROWB + n * (EPN * 4);
+            vo[e] = ksub * 32 * ROWB + r * ROWB + R::value_slot(r, 4 * e + 2 * half + ((i16 & 3) >> 1)) * 16 + (i16 & 1) * 8;
+    } else vo[0] = ksub * 32 * ROWB + 4 * h * ROWB + n * (EPN * 4);
 
     float w0 = 0.f, w1 = 0.f, w2 = 0.f;
     unsigned long long live0 = 0ull, live1 = 0ull;
@@ -139,11 +144,11 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[e][r] = 0.f;
 
-    auto compute = [&](auto buf_c, int t, float w) {
+    auto compute = [&](auto buf_c, int t, float w, int group) {      // groups group .. group + NS - 1 of the tile's keys (and ksub)
         constexpr int BUF = decltype(buf_c)::value;
-        const char* Kt = lds.rows[BUF][0];
-        const char* Vt = lds.rows[BUF][1];
-        const int k0 = t * kTileKeys + (NS == 1 ? 32 * ksub : 0);
+        const char* Kt = lds.rows[BUF][0] + group * (32 * ROWB);
+        const char* Vt = lds.rows[BUF][1] + group * (32 * ROWB);
+        const int k0 = t * kTileKeys + 32 * (ksub + group);
         // ---- logits, in units of 1 / scale
         __builtin_amdgcn_s_setprio(1);
         floatx16 s[NS];
@@ -176,7 +181,7 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
             const float x = w > 0.f ? __builtin_amdgcn_logf(w) * a.inv_scale : kTileDead;
 #pragma unroll
             for (int u = 0; u < NS; ++u) {
-                const float y = h == (NS == 1 ? ksub : u) ? x : 0.f;
+                const float y = h == ksub + group + u ? x : 0.f;
                 if constexpr (R::kB16) {
                     const unsigned int y0 = __float_as_uint(y) & 0xffff0000u;
                     const float rest = y - __uint_as_float(y0);
@@ -267,18 +272,28 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
             const bool more = t + 1 < t1;
             if (t + 2 < t1) w2 = weight(t + 2);
             live1 = more ? __ballot(w1 > 0.f) : 0ull;
-            if (live1 != 0ull) fetch(t + 1, BUF ^ 1);
-            if (has_rows && live0 != 0ull) compute(buf_c, t, w0);
+            if (BUFS == 2 && live1 != 0ull) fetch(t + 1, BUF ^ 1);
+            if (has_rows)
+                for (int i = 0; i < TIMES; ++i)
+                    if ((live0 >> (32 * (ksub + i)) & (NS == 2 ? ~0ull : 0xffffffffull)) != 0ull) compute(buf_c, t, w0, i);
             if (!more) return true;
+            if constexpr (BUFS == 1) {
+                tile_barrier();
+                if (live1 != 0ull) fetch(t + 1, 0);
+            }
             tile_arrived();
-            clear_dead(BUF ^ 1, live1);
+            clear_dead(BUFS == 2 ? BUF ^ 1 : 0, live1);
             tile_barrier();
             w0 = w1; w1 = w2; live0 = live1;
             return false;
         };
-        for (int t = t0;; t += 2) {
-            if (step(std::integral_constant<int, 0>{}, t)) break;
-            if (step(std::integral_constant<int, 1>{}, t + 1)) break;
+        if constexpr (BUFS == 2) {
+            for (int t = t0;; t += 2) {
+                if (step(std::integral_constant<int, 0>{}, t)) break;
+                if (step(std::integral_constant<int, 1>{}, t + 1)) break;
+            }
+        } else {
+            for (int t = t0; !step(std::integral_constant<int, 0>{}, t); ++t) {}
         }
     }
     l = half_sum(l);
@@ -358,7 +373,7 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kTileThreads, sizeof(T) == 2 ? 2 : 1) void tile_kernel(const TileArgs a) {
+__global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(const TileArgs a) {
     __shared__ TileLds<T, D> lds;
     // workgroup -> (job, cache, split, query tile); the query tiles of a split go to one XCD (blocks are dealt out to the eight
     // of them in turn), whose L2 then serves all but the first read of its rows
@@ -453,23 +468,26 @@ static int tile_qw(int64_t rows) { return rows > 64 ? 4 : rows > 32 ? 2 : 1; }
 static int64_t tile_units(int64_t n_streams, int64_t rows, int qw) { return n_streams * ((rows + 32 * qw - 1) / (32 * qw)); }
 
 // Splits of a job of this shape at most (any token count; with fewer queries to a workgroup there are more workgroups, and fewer splits).
-int tile_most_splits(int64_t n_streams, int64_t rows) {
+// Causal jobs in fp32 are cut twice as fine, as about half of their workgroups have little or nothing to do (1235 x 4 queries on 1235
+// tokens, 3 sequences, d = 128: 97 -> 75 us; bf16, whose cuts cost more than their work, 3156 x 4 queries: 60 -> 68).
+static int64_t tile_target(int elem, bool causal) { return elem == 4 && causal ? 2 * kTileTarget : kTileTarget; }
+int tile_most_splits(int64_t n_streams, int64_t rows, int elem, bool causal) {
     const int64_t wgs = tile_units(n_streams, rows, tile_qw(rows));
-    return wgs > 0 ? (int)max((int64_t)1, kTileTarget / wgs) : 1;
+    return wgs > 0 ? (int)max((int64_t)1, tile_target(elem, causal) / wgs) : 1;
 }
 
 // Queries of a workgroup and cuts of the keys.  Workgroups of 128 queries read the fewest keys; where they do not give every compute
 // unit one even with the keys cut, smaller ones are taken.  A cut of a workgroup of 128 queries costs 128 rows of sums written and
 // read, on bf16 about what two tiles of 64 keys take, so it gets eight of those where there are workgroups enough (in fp32 a tile takes
 // four times as long and no minimum is kept).  taken: workgroups of the launch that others have.
-void tile_plan(TileJob& j, int elem, int64_t taken) {
+void tile_plan(TileJob& j, int elem, bool causal, int64_t taken) {
     const int tiles = (j.count + kTileKeys - 1) / kTileKeys;
     for (j.qw = tile_qw(j.rows);; j.qw /= 2) {
         const int64_t wgs = tile_units(j.n_streams, j.rows, j.qw);
         j.n_qt = (j.rows + 32 * j.qw - 1) / (32 * j.qw);
         // (A few others that the chip has no place for beside these cost a second round: 512 + 32 workgroups, two a compute unit, 11.6 us,
         // 256 + 32 of them with twice the keys 7.7.  Many others are the launch's work themselves.)
-        int64_t splits = (kTileTarget - (taken <= kTileTarget / 8 ? taken : 0)) / wgs;
+        int64_t splits = (tile_target(elem, causal) - (taken <= kTileTarget / 8 ? taken : 0)) / wgs;
         if (j.qw == 4 && elem == 2) splits = min(splits, max((int64_t)(tiles + 7) / 8, (kTileFull + wgs - 1) / wgs));
         splits = max((int64_t)1, min(splits, (int64_t)tiles));
         j.tiles_per_split = (int)((tiles + splits - 1) / splits);
