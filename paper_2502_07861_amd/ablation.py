@@ -1,6 +1,6 @@
 """Ablation grid of the paper's single-layer study on synthetic data (one GPU).
 
-    python -m paper_2502_07861_amd.ablation [--seeds 10] [--json] [--recipe clustered|iid] [--value-factor | --value-augment | --alg1]
+    python -m paper_2502_07861_amd.ablation [--seeds 10] [--json] [--recipe clustered|iid] [--value-factor | --value-augment | --alg1 | --evict]
 
 For block sizes b in {256, 128, 64} and compression rates 2^-T in {1/2, 1/4, 1/8} (the grid of the runtime /
 relative-error tables in "Ablation Studies on Single Layer Attention Approximation", arXiv 2502.07861): the first
@@ -21,7 +21,9 @@ ln c per recipe and block size was bisected once on the CPU oracle (oracle/tunin
 four blocks of the first two sequences) so that the walk's decisions depend on the kernel weights.  --value-factor: the walk's weights carry the
 value factor <v_i,v_j>/r_value^2 of Alg. 2 line 6 (the numerator instance of Alg. 1 selects the kept set), with its own
 ln c per block size found the same way.  --value-augment (clustered recipe): the walk sees the value [v / r_value ; 1], i.e. the
-factor (<v_i,v_j>/r_value^2 + 1) / 2: one kept set chosen for numerator and denominator together.
+factor (<v_i,v_j>/r_value^2 + 1) / 2: one kept set chosen for numerator and denominator together.  --evict: next to both, eviction by
+accumulated attention weight at the same budget: half of the queries judge the tokens (`bkv_attend_mass`), the heaviest stay beside the
+windows with their own weights (`bkv_evict`), and all kept sets answer the other half.
 """
 from __future__ import annotations
 
@@ -205,6 +207,55 @@ def run_alg1(seeds=5, block=128, rounds=ROUNDS, n=8192, n_seq=8, device="cuda", 
                          % (n_seq, n, d, nq), seeds=seeds, rows=rows)
 
 
+def run_evict(seeds=5, block=128, rounds=ROUNDS, n_mid=N_MID, n_seq=8, device="cuda", nq=64, recipe="clustered", keep_outputs=False):
+    """Eviction by accumulated attention weight beside the halving tree and uniform sampling, at equal numbers of kept tokens.  The first
+    half of the queries of every head judges, the second half asks; errors are over the asking ones.  Eviction draws nothing: one run."""
+    K, V, Q = make_inputs(device, n_seq=n_seq, n_mid=n_mid, nq=nq, recipe=recipe)
+    n, d = K.shape[1], K.shape[2]
+    judge, ask = Q[:, :, :nq // 2].contiguous(), Q[:, :, nq // 2:].contiguous()
+    exact, _ = exact_attention_f64(K, V, ask)
+    ones = torch.ones(n_seq, n, device=device)
+    rows = []
+    for T in rounds:
+        acc = dict(tree=[], uniform=[], tree_ms=[], evict_ms=[])
+        for s in range(seeds + 1):                          # run 0 warms up and is not counted
+            p = binding.make_params(d, block, T, K.dtype, log_c=log_c_for(recipe, block), seed=1000 + s, center=True)
+            ev = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
+            ev[0].record()
+            tree = binding.merge_reduce_protected(p, K, V, N_SINK, N_RECENT)
+            ev[1].record()
+            mass = binding.attend_mass(p, K, V, ones, judge)[2]
+            heavy = binding.evict(p, K, V, ones, mass, tree["K"].shape[1], n_sink=N_SINK, n_recent=N_RECENT)
+            ev[2].record()
+            z, _ = binding.attend_kv(p, tree["K"], tree["V"], tree["w"], ask)
+            ze, _ = binding.attend_kv(p, heavy["K"], heavy["V"], heavy["w"], ask)
+            idx_u, w_u = uniform_sample_protected(n_seq, n, N_SINK, N_RECENT, T, 7000 + s, device)
+            gi = idx_u[..., None].expand(-1, -1, d)
+            zu, _ = binding.attend_kv(p, torch.gather(K, 1, gi), torch.gather(V, 1, gi), w_u, ask)
+            torch.cuda.synchronize()
+            if s == 0:
+                continue
+            acc["tree"].append(relative_error(z, exact)); acc["uniform"].append(relative_error(zu, exact))
+            acc["tree_ms"].append(ev[0].elapsed_time(ev[1])); acc["evict_ms"].append(ev[1].elapsed_time(ev[2]))
+        m = {k: float(torch.tensor(v).mean()) for k, v in acc.items()}
+        m.update({k + "_std": _std(torch.tensor(acc[k])) for k in ("tree", "uniform")})
+        m.update(rate="1/%d" % (1 << T), block=block, kept=int(tree["K"].shape[1]), evict=relative_error(ze, exact))
+        if keep_outputs:
+            m["last"] = dict(mass=mass, idx=heavy["idx"], w=heavy["w"], z=ze)
+        rows.append(m)
+    return dict(workload="%d KV sequences x (%d + %d + %d) tokens, d=%d, %d x %d judging and as many asking queries, bf16, synthetic (recipe %s)"
+                         % (n_seq, N_SINK, n_mid, N_RECENT, d, Q.shape[1], judge.shape[2], recipe), seeds=seeds, rows=rows,
+                **(dict(K=K, V=V, judge=judge, ask=ask, exact=exact) if keep_outputs else {}))
+
+
+def evict_table(result):
+    lines = ["| block | rate | kept | tree ms | mass + evict ms | BalanceKV rel. err | eviction rel. err | uniform rel. err |", "|---|---|---|---|---|---|---|---|"]
+    for r in result["rows"]:
+        lines.append("| %d | %s | %d | %.3f | %.3f | %.4f ± %.4f | %.4f | %.4f ± %.4f |"
+                     % (r["block"], r["rate"], r["kept"], r["tree_ms"], r["evict_ms"], r["tree"], r["tree_std"], r["evict"], r["uniform"], r["uniform_std"]))
+    return "\n".join(lines)
+
+
 def alg1_table(result):
     lines = ["| block | rate | kept (numerator / denominator set) | build sets ms | two-set attend ms | Alg. 1 rel. err | one keys-only set | uniform |",
              "|---|---|---|---|---|---|---|---|"]
@@ -233,6 +284,7 @@ def main(argv=None):
     ap.add_argument("--value-factor", action="store_true", help="kernel weights times <v_i,v_j>/r_value^2 (Alg. 2 line 6)")
     ap.add_argument("--value-augment", action="store_true", help="kernel weights times (<v_i,v_j>/r_value^2 + 1) / 2: the value [v / r ; 1]")
     ap.add_argument("--alg1", action="store_true", help="Alg. 1 as listed (buckets, two kept sets) on heavy-tailed value norms")
+    ap.add_argument("--evict", action="store_true", help="eviction by accumulated attention weight beside the tree and uniform sampling")
     ap.add_argument("--recipe", default="clustered", choices=["clustered", "iid"], help="input recipe of the grid")
     args = ap.parse_args(argv)
     if not torch.cuda.is_available():
@@ -242,6 +294,10 @@ def main(argv=None):
     if args.alg1:
         result = run_alg1(seeds=args.seeds)
         print(json.dumps(result) if args.json else result["workload"] + ", %d seeds\n" % result["seeds"] + alg1_table(result))
+        return 0
+    if args.evict:
+        result = run_evict(seeds=args.seeds, recipe=args.recipe)
+        print(json.dumps(result) if args.json else result["workload"] + ", %d seeds\n" % result["seeds"] + evict_table(result))
         return 0
     result = run(seeds=args.seeds, value_gram=args.value_factor, recipe=args.recipe, value_augment=args.value_augment)
     if args.json:

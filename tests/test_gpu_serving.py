@@ -397,3 +397,22 @@ def test_caches_of_the_streaming_handle(bk):
     cache.load(kept["K"], kept["V"], kept["w"])
     assert cache.count == 100
     cache.close()
+
+
+def test_ablation_compares_eviction(bk):
+    """The study's eviction columns: the kept sets by the formulas, the estimate over them, and the error formula on top."""
+    from paper_2502_07861_amd import ablation
+    res = ablation.run_evict(seeds=1, n_mid=1024, n_seq=2, nq=8, rounds=(1, 2), keep_outputs=True)
+    n, q = res["K"].shape[1], res["judge"].reshape(2, -1, 128)
+    ones = torch.ones(n, device="cuda")
+    for row in res["rows"]:
+        last = row["last"]
+        for s in range(2):
+            ref = _attention(q[s], res["K"][s], res["V"][s], ones)
+            _check_mass(last["mass"][s], last["mass"][s], 0.0, ref, n, 16, "sequence %d" % s)
+            kept = _kept(ones, last["mass"][s], n, row["kept"], ablation.N_SINK, ablation.N_RECENT)
+            assert last["idx"][s].tolist() == kept.tolist()
+            at = torch.from_numpy(kept).cuda()
+            _check_out(last["z"][s], None, _attention(res["ask"][s].reshape(-1, 128), res["K"][s][at], res["V"][s][at], ones[at]), BF16, len(kept), "rate " + row["rate"])
+        assert row["kept"] == 512 + (1024 >> (1 if row["rate"] == "1/2" else 2)) and row["evict"] == ablation.relative_error(last["z"], res["exact"])
+    assert len(ablation.evict_table(res).splitlines()) == 4
