@@ -216,8 +216,10 @@ int bkv_attend_kv_static(const bkv_params* p, const void* K_c, const void* V_c, 
  *               A count may be 0 (its pointers are then not looked at).  A place whose weight is not above 0 holds no token,
  *               whatever its rows hold (infinities and NaN too): sequences of different lengths share a count that way.
  * Q, out, lse_out  as in bkv_attend_kv; out must not overlap Q.  A query that meets no token gives zeros and lse = -inf.
- * Precision as in bkv_attend_kv.  The workspace may hold anything; calls that overlap in time must not share one.
- * Limits: n_seq <= 65535, g * nq <= 262140, n_seq * g * nq < 2^31, counts <= 2^30 (else BKV_ESHAPE).                        */
+ * Precision as in bkv_attend_kv, but with BKV_BF16 and more than 64 queries on a cache (a prefix's are those of all its
+ * sequences) a weight may multiply its value row as one bf16 number (relative error <= 2^-8); lse_out is not affected.
+ * The workspace may hold anything; calls that overlap in time must not share one.
+ * Limits: n_seq <= 65535, g * nq <= 262140, n_seq * g * nq <= 2^31 - 256, counts <= 2^30 (else BKV_ESHAPE).                 */
 size_t bkv_attend_prefix_workspace_bytes(const bkv_params* p, int64_t n_pre, int64_t n_seq, int32_t g,
                                          int32_t nq);   /* for any counts */
 int bkv_attend_prefix(const bkv_params* p, const void* K_p, const void* V_p, const float* w_p, int64_t n_pre,
@@ -233,7 +235,8 @@ int bkv_attend_prefix(const bkv_params* p, const void* K_p, const void* V_p, con
  * too: their P is 0).
  * visible       query i (0 <= i < nq) of every head sees the first visible + i places (none where that is not above 0); from
  *               `count` on all see everything.  The last nq tokens of a cache against it: count - nq + 1; a prompt against
- *               itself: 1.
+ *               itself: 1.  What places hold that no query sees does not matter; value rows of tokens that some queries see
+ *               must be finite, as those that do not see them add them with weight 0.
  * mass_in       [n_seq, stride_tokens] fp32 or NULL (zeros); may be mass_out, no other overlap.  decay in [0, 1]; with 0 it is
  *               not read.  mass_out [n_seq, stride_tokens]: places from `count` on are left as they are.  count == 0: untouched.
  * The sums run in an order that depends on the shapes alone: the same call gives the same bits.                             */

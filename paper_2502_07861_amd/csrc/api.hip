@@ -432,12 +432,12 @@ static void tile_common(bkv::TileArgs& a, const bkv_params* p, const void* Q, vo
     a.inv_scale = (float)(sqrt((double)p->d) / 1.4426950408889634);
 }
 
-// Shapes that every attention of this section takes: what attend_kv takes, with at most 2^31 - 1 queries in all.
+// Shapes that every attention of this section takes: what attend_kv takes, with at most 2^31 - 256 queries in all.
 static int check_queries(const bkv_params* p, int64_t n_seq, int32_t g, int32_t nq) {
     const int rc = check_params(p);
     if (rc) return rc;
     if (n_seq < 0 || g <= 0 || nq <= 0) return BKV_EINVAL;
-    if (n_seq > 65535 || (int64_t)g * nq > 4 * 65535 || n_seq * g * nq > 0x7fffffffll) return BKV_ESHAPE;
+    if (n_seq > 65535 || (int64_t)g * nq > 4 * 65535 || n_seq * g * nq > 0x7fffff00ll) return BKV_ESHAPE;
     return BKV_OK;
 }
 

@@ -140,7 +140,7 @@ __global__ __launch_bounds__(kMassThreads, sizeof(T) == 2 ? 3 : 1) void mass_ker
         }
     };
     if (t < tiles) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0), in the compiler's books too
+        all_arrived_so_far();
         tile_barrier();
         auto step = [&](auto buf_c) {            // true: this was the last tile
             constexpr int BUF = decltype(buf_c)::value;

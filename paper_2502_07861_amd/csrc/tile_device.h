@@ -67,6 +67,11 @@ __device__ __forceinline__ void to_lds(const char* base, unsigned int off, unsig
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
 }
 __device__ __forceinline__ void tile_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// The same in the compiler's books too (which hold the loads it made itself): nothing behind it waits for those again.
+__device__ __forceinline__ void all_arrived_so_far() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
+    tile_arrived();
+}
 // All wavefronts' LDS writes are done and seen: loads under way stay so (a __syncthreads would wait for them).
 __device__ __forceinline__ void tile_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");

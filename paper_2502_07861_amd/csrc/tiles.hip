@@ -52,11 +52,12 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
     const int tiles = (J.count + kTileKeys - 1) / kTileKeys;
     const int t0 = split * J.tiles_per_split;
     int t1 = min(tiles, t0 + J.tiles_per_split);
-    int sees = J.count, sees_min = J.count;
+    int sees = J.count, sees_min = J.count, most = J.count;          // places: that this query, any one of the wavefront, one of the workgroup sees
     if (a.causal) {
         auto visible = [&](int i) { return (int)min((int64_t)J.count, max((int64_t)0, a.visible + i)); };
         sees = visible(outer);
-        t1 = min(t1, (visible((min(row_first + 32 * QW, J.rows) - 1) / J.inner) + kTileKeys - 1) / kTileKeys);
+        most = visible((min(row_first + 32 * QW, J.rows) - 1) / J.inner);
+        t1 = min(t1, (most + kTileKeys - 1) / kTileKeys);
         sees_min = visible(min(row0, J.rows - 1) / J.inner);
     }
 
@@ -94,7 +95,7 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
     auto weight = [&](int t) {                                       // lane: key
         const int key = t * kTileKeys + lane;
         const float w = wb[min(key, J.count - 1)];
-        return key < J.count ? w : 0.f;
+        return key < most ? w : 0.f;
     };
     // rows of places without a token, whatever they hold: 0 (each wavefront those it brought)
     auto clear_dead = [&](int buf, unsigned long long live) {
@@ -262,7 +263,7 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
     };
 
     if (t0 < t1) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0), in the compiler's books too: nothing in the loop waits for the queries again
+        all_arrived_so_far();
         live0 = __ballot(w0 > 0.f);
         clear_dead(0, live0);
         tile_barrier();

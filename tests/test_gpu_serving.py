@@ -139,7 +139,8 @@ MASS = [  # dtype, d, n_seq, count, g, nq, visible, decay
     (BF16, 128, 1, 128, 1, 5000, None, 0.25), (BF16, 64, 70, 300, 1, 1, None, 1.0), (BF16, 128, 1, 3000, 1, 300, 2701, 1.0),
     (F32, 64, 1, 1, 1, 1, None, 1.0), (F32, 128, 2, 130, 4, 1, None, 0.5), (F32, 64, 2, 333, 2, 37, -4, 0.5), (F32, 128, 1, 200, 2, 200, 1, 0.0),
     (F32, 64, 3, 4097, 4, 1, None, 1.0), (F32, 128, 2, 500, 1, 130, 371, 0.9), (F32, 64, 1, 70, 7, 70, 1, 1.0), (BF16, 128, 2, 500, 2, 10, -1000, 1.0),
-    (BF16, 128, 2, 40, 2, 90, 1, 1.0),
+    (BF16, 128, 2, 40, 2, 90, 1, 1.0), (BF16, 128, 9, 250, 3, 250, 1, 1.0), (BF16, 64, 50, 140, 2, 70, 71, 0.5), (F32, 128, 9, 150, 2, 100, 51, 1.0),
+    (BF16, 128, 3, 2000, 1, 500, 1501, 1.0), (BF16, 64, 1, 640, 8, 640, -3, 0.0),
 ]
 
 
@@ -179,6 +180,19 @@ def test_mass(bk, dtype, d, n_seq, count, g, nq, visible, decay):
     fresh = bk.attend_mass(p, K, V, w, Q, count=count, visible=visible)[2]
     zero = bk.attend_mass(p, K, V, w, Q, before, count=count, visible=visible, decay=0.0)[2]
     assert torch.equal(fresh, zero) and bool((fresh[:, count:] == 0).all())
+
+
+@pytest.mark.parametrize("g,nq", [(2, 3), (4, 40)])
+def test_places_that_no_query_sees_do_not_matter(bk, g, nq):
+    gen = _gen(12)
+    K, V, w = _cache(gen, 2, 300, 128, BF16)
+    Q = torch.randn(2, g, nq, 128, generator=gen, device="cuda").to(BF16)
+    p = bk.make_params(128, 64, 1, BF16, log_c=0.0)
+    seen = 100 + nq - 1
+    ref = bk.attend_mass(p, K, V, w, Q, visible=100)
+    K[:, seen:], V[:, seen:] = float("nan"), float("inf")
+    got = bk.attend_mass(p, K, V, w, Q, visible=100)
+    assert all(torch.equal(a, b) for a, b in zip(got, ref)) and bool((got[2][:, seen:] == 0).all())
 
 
 def test_mass_adds_up_to_the_queries(bk):
