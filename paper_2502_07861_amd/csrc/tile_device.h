@@ -25,16 +25,16 @@ template <typename T, int D> struct TileRows {
     static constexpr int kSlots = kRowB / 16;             // 16-byte slots of a row
     static constexpr int kPieces = kRowB / 32;            // contraction pieces of a row
     static constexpr int kEpn = D / 32;                   // product tiles along the head dimension
-    // Rows are whole multiples of half the LDS banks, so slot s of row r is stored at another place: 8 (or 16) rows read at one
-    // slot, and 8 rows read at two neighbouring slots by the transposing read, then meet different banks.
+    // Rows are whole multiples of half the LDS banks, so slot s of row r is stored at another place: 16 rows read at one slot (keys), and
+    // four rows read at four neighbouring slots by 32 lanes of the transposing read (values), then meet different banks.
     static __device__ __forceinline__ int key_slot(int r, int s) {
         if constexpr (kRowB == 128) return s ^ ((r >> 1) & 7);
         else return s ^ (r & 15);
     }
     static __device__ __forceinline__ int value_slot(int r, int s) {
         if constexpr (!kB16) return s;
-        else if constexpr (kRowB == 128) return s ^ (((r >> 1) & 3) << 1);
-        else return s ^ ((r & 7) << 1);
+        else if constexpr (kRowB == 128) return s ^ (((r >> 1) & 1) << 2);
+        else return s ^ ((r & 3) << 2);
     }
 };
 
