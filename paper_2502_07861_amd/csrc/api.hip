@@ -540,6 +540,10 @@ int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const
     j.n_streams = (int32_t)n_seq; j.rows = n_q; j.inner = g; j.q_stream = n_q; j.q_outer = 1; j.q_inner = nq;
     a.causal = visible < count;
     a.visible = visible < -(int64_t)nq ? -(int64_t)nq : visible;
+    if (a.causal) {                                        // the pass: places that some query sees
+        const int64_t seen = a.visible + nq - 1;
+        j.count = (int32_t)(seen < 0 ? 0 : seen < count ? seen : count);
+    }
     char* ws = (char*)workspace;
     a.stats = (float*)ws;
     ws += align_up((size_t)n_seq * n_q * 8, 256);

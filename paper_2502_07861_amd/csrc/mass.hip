@@ -199,10 +199,11 @@ size_t mass_part_bytes() { return (size_t)kMassTarget * kMassKeys * sizeof(float
 static int mass_splits(int64_t n_seq, int64_t count, int64_t rows, int elem) {
     const int64_t wgs = n_seq * ((count + kMassKeys - 1) / kMassKeys);
     // (bf16: a workgroup takes the time of two or three tiles to begin and to end: eight tiles each, where there are workgroups enough.
-    // fp32: a tile takes longer than that by itself.)
+    // fp32: a tile takes longer than that by itself.  Three tiles or fewer are over before another launch would have added them up.)
     const int64_t tiles = (rows + kMassRows - 1) / kMassRows, fill = (256 + wgs - 1) / wgs;
     int64_t most = elem == 2 ? tiles / 8 > fill ? tiles / 8 : fill : tiles;
     if (most > tiles) most = tiles;
+    if (tiles < 4) most = 1;
     int64_t splits = (elem == 2 ? kMassTarget : kMassTarget / 2) / wgs;
     if (splits > most) splits = most;
     return splits < 1 ? 1 : (int)splits;
