@@ -244,8 +244,9 @@ struct TileJob {
     int64_t stride;
     int64_t q_stream, q_outer, q_inner;
     int32_t count, n_streams, rows, inner;
-    // set by tile_plan: query tiles of 32 that a workgroup takes, workgroups per cache and split, splits, tiles of keys in one
-    int32_t qw, n_qt, splits, tiles_per_split, by_xcd;
+    // set by tile_plan: query tiles of 32 that a workgroup takes (0: caches a wavefront each), workgroups per cache and split, splits, tiles
+    // of keys in one, caches times splits (0: workgroups)
+    int32_t qw, n_qt, splits, tiles_per_split, units, by_xcd;
     float* part;              // set by the launcher: [splits, n_rows, d + pad], null: results are written
 };
 struct TileArgs {
@@ -261,7 +262,7 @@ struct TileArgs {
     uint32_t first;           // set by the launcher: workgroups of job 0
 };
 int tile_most_splits(int64_t n_streams, int64_t rows, int elem, bool causal);
-void tile_plan(TileJob& j, int elem, bool causal, int64_t taken);
+void tile_plan(TileJob& j, int row_bytes, int elem, bool causal, int64_t taken);
 size_t tile_part_bytes(int d, int64_t n_rows, int splits);
 // part: room for the partial rows of all splits of all jobs, if they are more than one
 hipError_t launch_tiles(int dtype, int d, TileArgs& a, int n_jobs, float* part, hipStream_t st);

@@ -25,15 +25,21 @@ template <typename T, int D> struct TileLds {
     __align__(16) char rows[kBuffers][2][kTileKeys * D * sizeof(T)];        // [buffer][keys, values]
 };
 
-// QW: wavefronts with queries of their own; 4 / QW share the same ones.
+// Short caches of many sequences: a wavefront each, 32 keys at a time, nothing shared; so many wavefronts of a workgroup have room in LDS.
+template <typename T, int D> constexpr int kSoloWaves = D * sizeof(T) == 512 ? 2 : 4;
+
+// QW: wavefronts with queries of their own; 4 / QW share the same ones.  0: a wavefront is on its own.
 template <typename T, int D, int QW>
-__device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, int64_t stream, int split, int qt, TileLds<T, D>& lds) {
+__device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, int64_t stream /* SOLO: a workgroup's */, int split, int qt, TileLds<T, D>& lds) {
     using R = TileRows<T, D>;
     using F = TileFetch<T, D>;
-    constexpr int ROWB = R::kRowB, EPN = R::kEpn, P = D + kTilePad, TILEB = kTileKeys * ROWB;
-    constexpr int BUFS = TileLds<T, D>::kBuffers;
+    constexpr int ROWB = R::kRowB, EPN = R::kEpn, P = D + kTilePad;
+    constexpr bool SOLO = QW == 0;
+    constexpr int Q1 = SOLO ? 1 : QW;
+    constexpr int KEYS = SOLO ? 32 : kTileKeys, TILEB = KEYS * ROWB, BUFS = SOLO ? 1 : TileLds<T, D>::kBuffers;
+    constexpr int SHARE = SOLO ? KEYS : KEYS / 4, STEPS = SHARE / F::kRps;        // rows of a tile that a wavefront brings
     // wavefronts a query has; groups of 32 keys a wavefront takes of a tile at a time, times (fp32: registers)
-    constexpr int KW = 4 / QW, NS = QW == 4 && R::kB16 ? 2 : 1, TIMES = QW == 4 ? 2 / NS : 1;
+    constexpr int KW = SOLO ? 1 : 4 / Q1, NS = QW == 4 && R::kB16 ? 2 : 1, TIMES = QW == 4 ? 2 / NS : 1;
     // bf16: a weight multiplies its value row as two bf16 numbers, its upper bits and what they leave (relative error 2^-17), except
     // for full workgroups of 128 queries, where the matrix cores are the bound: there it is rounded to one (2^-8), as the result is.
     // 8 prefixes x 16385 tokens x 1280 queries: 165 -> 137 us, off the 64-bit result 1.7e-3 -> 2.1e-3 (rounding it makes 1.7e-3).
@@ -41,23 +47,27 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
 
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int qsub = wave & (QW - 1), ksub = wave / QW;
+    const int qsub = SOLO ? 0 : wave & (Q1 - 1), ksub = SOLO ? 0 : wave / Q1;
+    if constexpr (SOLO) {
+        stream = stream * kSoloWaves<T, D> + wave;
+        if (wave >= kSoloWaves<T, D> || stream >= J.n_streams) return;          // (no barrier below)
+    }
     const int row_first = qt * 32 * QW, row0 = row_first + 32 * qsub;
-    const bool has_rows = row0 < J.rows && ksub * 32 < kTileKeys;
+    const bool has_rows = row0 < J.rows && ksub * 32 < KEYS;
     const int row = min(row0 + n, J.rows - 1);
     const int outer = row / J.inner;
     const int64_t q_row = stream * J.q_stream + (int64_t)outer * J.q_outer + (int64_t)(row - outer * J.inner) * J.q_inner;
 
     // tiles of keys of this workgroup
-    const int tiles = (J.count + kTileKeys - 1) / kTileKeys;
+    const int tiles = (J.count + KEYS - 1) / KEYS;
     const int t0 = split * J.tiles_per_split;
     int t1 = min(tiles, t0 + J.tiles_per_split);
     int sees = J.count, sees_min = J.count, most = J.count;          // places: that this query, any one of the wavefront, one of the workgroup sees
     if (a.causal) {
         auto visible = [&](int i) { return (int)min((int64_t)J.count, max((int64_t)0, a.visible + i)); };
         sees = visible(outer);
-        most = visible((min(row_first + 32 * QW, J.rows) - 1) / J.inner);
-        t1 = min(t1, (most + kTileKeys - 1) / kTileKeys);
+        most = visible((min(row_first + 32 * Q1, J.rows) - 1) / J.inner);
+        t1 = min(t1, (most + KEYS - 1) / KEYS);
         sees_min = visible(min(row0, J.rows - 1) / J.inner);
     }
 
@@ -66,47 +76,49 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
     const float* wb = J.w + (size_t)stream * J.stride;
 
     // ---- a tile on its way: this lane's bytes of each step, the slots exchanged as the rows are stored
-    unsigned int kgo[F::kSteps], vgo[F::kSteps];
+    const int share0 = SOLO ? 0 : SHARE * wave;
+    unsigned int kgo[STEPS], vgo[STEPS];
 #pragma unroll
-    for (int i = 0; i < F::kSteps; ++i) {
-        const int r = 16 * wave + F::row(i, lane), s = lane % R::kSlots;
+    for (int i = 0; i < STEPS; ++i) {
+        const int r = share0 + F::row(i, lane), s = lane % R::kSlots;
         kgo[i] = r * ROWB + R::key_slot(r, s) * 16;
         vgo[i] = r * ROWB + R::value_slot(r, s) * 16;
     }
-    const unsigned int lds0 = lds_address(&lds.rows[0][0][0]) + 16 * wave * ROWB;
+    char* mine = &lds.rows[0][0][0] + (SOLO ? wave * 2 * TILEB : 0);           // [buffer][keys, values] of this wavefront or workgroup
+    const unsigned int lds0 = lds_address(mine) + share0 * ROWB;
     auto fetch = [&](int t, int buf) {
         const char* kp = Kb + (size_t)t * TILEB;
         const char* vp = Vb + (size_t)t * TILEB;
         const unsigned int to = lds0 + buf * 2 * TILEB;
-        const int left = J.count - 1 - t * kTileKeys;                // last row there is
-        if (left >= kTileKeys - 1) {
+        const int left = J.count - 1 - t * KEYS;                     // last row there is
+        if (left >= KEYS - 1) {
 #pragma unroll
-            for (int i = 0; i < F::kSteps; ++i) { to_lds(kp, kgo[i], to + 1024 * i); to_lds(vp, vgo[i], to + TILEB + 1024 * i); }
+            for (int i = 0; i < STEPS; ++i) { to_lds(kp, kgo[i], to + 1024 * i); to_lds(vp, vgo[i], to + TILEB + 1024 * i); }
         } else {                                                     // (rows past the end repeat it, with weight 0)
 #pragma unroll
-            for (int i = 0; i < F::kSteps; ++i) {
-                const int r = 16 * wave + F::row(i, lane);
+            for (int i = 0; i < STEPS; ++i) {
+                const int r = share0 + F::row(i, lane);
                 const unsigned int back = max(r - left, 0) * ROWB;
                 to_lds(kp, kgo[i] - back, to + 1024 * i);
                 to_lds(vp, vgo[i] - back, to + TILEB + 1024 * i);
             }
         }
     };
-    auto weight = [&](int t) {                                       // lane: key
-        const int key = t * kTileKeys + lane;
+    auto weight = [&](int t) {                                       // lane (SOLO: and lane + 32): key
+        const int key = t * KEYS + (lane & (KEYS - 1));
         const float w = wb[min(key, J.count - 1)];
         return key < most ? w : 0.f;
     };
     // rows of places without a token, whatever they hold: 0 (each wavefront those it brought)
     auto clear_dead = [&](int buf, unsigned long long live) {
-        unsigned int dead = (unsigned int)(~live >> (16 * wave)) & 0xffffu;
+        unsigned int dead = (unsigned int)(~live >> share0) & (SOLO ? 0xffffffffu : 0xffffu);
         if (live == 0ull) return;                                    // (not fetched, not looked at)
         while (dead != 0u) {
-            const int r = 16 * wave + __builtin_ctz(dead);
+            const int r = share0 + __builtin_ctz(dead);
             dead &= dead - 1u;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                char* to = &lds.rows[buf][k][r * ROWB + lane * (ROWB / 64)];
+                char* to = mine + (2 * buf + k) * TILEB + r * ROWB + lane * (ROWB / 64);
                 if constexpr (ROWB == 128) *reinterpret_cast<unsigned short*>(to) = 0;
                 else if constexpr (ROWB == 256) *reinterpret_cast<unsigned int*>(to) = 0u;
                 else *reinterpret_cast<uint2*>(to) = make_uint2(0u, 0u);
@@ -147,9 +159,9 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
 
     auto compute = [&](auto buf_c, int t, float w, int group) {      // groups group .. group + NS - 1 of the tile's keys (and ksub)
         constexpr int BUF = decltype(buf_c)::value;
-        const char* Kt = lds.rows[BUF][0] + group * (32 * ROWB);
-        const char* Vt = lds.rows[BUF][1] + group * (32 * ROWB);
-        const int k0 = t * kTileKeys + 32 * (ksub + group);
+        const char* Kt = mine + 2 * BUF * TILEB + group * (32 * ROWB);
+        const char* Vt = Kt + TILEB;
+        const int k0 = t * KEYS + 32 * (ksub + group);
         // ---- logits, in units of 1 / scale
         __builtin_amdgcn_s_setprio(1);
         floatx16 s[NS];
@@ -262,11 +274,15 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
         }
     };
 
+    auto barrier = [] {
+        if constexpr (SOLO) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        else tile_barrier();
+    };
     if (t0 < t1) {
         all_arrived_so_far();
         live0 = __ballot(w0 > 0.f);
         clear_dead(0, live0);
-        tile_barrier();
+        barrier();
         // one tile: the next one is requested, this one multiplied, the next one awaited; true: this was the last one
         auto step = [&](auto buf_c, int t) {
             constexpr int BUF = decltype(buf_c)::value;
@@ -279,12 +295,12 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
                     if ((live0 >> (32 * (ksub + i)) & (NS == 2 ? ~0ull : 0xffffffffull)) != 0ull) compute(buf_c, t, w0, i);
             if (!more) return true;
             if constexpr (BUFS == 1) {
-                tile_barrier();
+                barrier();
                 if (live1 != 0ull) fetch(t + 1, 0);
             }
             tile_arrived();
             clear_dead(BUFS == 2 ? BUF ^ 1 : 0, live1);
-            tile_barrier();
+            barrier();
             w0 = w1; w1 = w2; live0 = live1;
             return false;
         };
@@ -382,7 +398,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(const TileArgs a)
     const int which = block >= a.first ? 1 : 0;
     block -= which ? a.first : 0u;
     const TileJob J = which ? a.job[1] : a.job[0];
-    const unsigned int units = (unsigned int)J.n_streams * (unsigned int)J.splits, in_xcd = block >> 3;
+    const unsigned int units = (unsigned int)J.units, in_xcd = block >> 3;
     const unsigned int unit = J.by_xcd ? in_xcd / (unsigned int)J.n_qt * 8u + (block & 7u) : block % units;
     const unsigned int turn = J.by_xcd ? in_xcd % (unsigned int)J.n_qt : block / units;
     if (unit >= units || turn >= (unsigned int)J.n_qt) return;
@@ -391,7 +407,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(const TileArgs a)
     const int64_t stream = unit / (unsigned int)J.splits;
     if (J.qw == 4) tile_body<T, D, 4>(a, J, stream, split, qt, lds);
     else if (J.qw == 2) tile_body<T, D, 2>(a, J, stream, split, qt, lds);
-    else tile_body<T, D, 1>(a, J, stream, split, qt, lds);
+    else if (J.qw == 1) tile_body<T, D, 1>(a, J, stream, split, qt, lds);
+    else tile_body<T, D, 0>(a, J, stream, split, qt, lds);
 }
 
 // Partial rows of all splits of a query -> its result.  D / 4 lanes a query, four columns each; SG groups of lanes take its splits in
@@ -481,7 +498,7 @@ int tile_most_splits(int64_t n_streams, int64_t rows, int elem, bool causal) {
 // unit one even with the keys cut, smaller ones are taken.  A cut of a workgroup of 128 queries costs 128 rows of sums written and
 // read, on bf16 about what two tiles of 64 keys take, so it gets eight of those where there are workgroups enough (in fp32 a tile takes
 // four times as long and no minimum is kept).  taken: workgroups of the launch that others have.
-void tile_plan(TileJob& j, int elem, bool causal, int64_t taken) {
+void tile_plan(TileJob& j, int row_bytes, int elem, bool causal, int64_t taken) {
     const int tiles = (j.count + kTileKeys - 1) / kTileKeys;
     for (j.qw = tile_qw(j.rows);; j.qw /= 2) {
         const int64_t wgs = tile_units(j.n_streams, j.rows, j.qw);
@@ -496,8 +513,16 @@ void tile_plan(TileJob& j, int elem, bool causal, int64_t taken) {
         if (j.qw == 1 || wgs * j.splits >= kTileFull * 3 / 4) break;
     }
     // XCDs take the query tiles of a split each where that gives them equal shares, else whatever comes next
-    const int64_t units = (int64_t)j.n_streams * j.splits;
-    j.by_xcd = units % 8 == 0 || units >= 48;
+    j.units = j.n_streams * j.splits;
+    // More short sequences of at most 32 queries than a round of workgroups has places: a wavefront each, which waits for nobody (call
+    // times, a workgroup each beside: 7232 x 3 keys on 113 prefixes x 195 bf16 81 -> 35 us; 4096 x 60 keys bf16 56 -> 34, fp32 111 -> 87,
+    // x 250 fp32 348 -> 296, bf16 123 -> 115; but 320 x 250 16.4 -> 20.9, the chip half empty and the keys one after the other).
+    if (j.rows <= 32 && j.n_streams > kTileTarget / 2 && j.count <= (j.n_streams >= 2 * kTileTarget ? 256 : 128)) {
+        const int per = row_bytes == 512 ? 2 : 4;
+        j.qw = 0; j.n_qt = 1; j.splits = 1; j.tiles_per_split = 8;             // (tiles of 32 keys)
+        j.units = (j.n_streams + per - 1) / per;
+    }
+    j.by_xcd = j.units % 8 == 0 || j.units >= 48;
 }
 
 size_t tile_part_bytes(int d, int64_t n_rows, int splits) { return (size_t)n_rows * splits * (d + kTilePad) * sizeof(float); }
@@ -509,7 +534,7 @@ static hipError_t launch_tiles_t(TileArgs& a, int n_jobs, float* part, hipStream
     for (int k = 0; k < n_jobs; ++k) {
         TileJob& j = a.job[k];
         if (k == 1) a.first = (uint32_t)blocks;
-        const uint64_t own = (uint64_t)j.n_streams * j.splits;
+        const uint64_t own = (uint64_t)j.units;
         blocks += j.by_xcd ? (own + 7) / 8 * 8 * j.n_qt : (own * j.n_qt + 7) / 8 * 8;
         units += (uint64_t)j.n_streams * j.count;
         splits += j.splits;

@@ -432,3 +432,20 @@ def test_ablation_compares_eviction(bk):
             _check_out(last["z"][s], None, _attention(res["ask"][s].reshape(-1, 128), res["K"][s][at], res["V"][s][at], ones[at]), BF16, len(kept), "rate " + row["rate"])
         assert row["kept"] == 512 + (1024 >> (1 if row["rate"] == "1/2" else 2)) and row["evict"] == ablation.relative_error(last["z"], res["exact"])
     assert len(ablation.evict_table(res).splitlines()) == 4
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("g,cs", [(1, 1), (4, 31), (3, 32), (32, 33), (5, 64), (8, 127), (2, 255)])
+def test_prefix_many_sequences_of_few_tokens(bk, dtype, d, g, cs):
+    """More sequences than compute units, a few own tokens each, some of them absent, some sequences without one."""
+    gen, n_pre, fan, cp = _gen(g + cs), 3, 101 if cs < 128 else 342, 70
+    pre, own = _cache(gen, n_pre, cp, d, dtype), _cache(gen, n_pre * fan, cs + 1, d, dtype)
+    own[2][5:9], own[0][5:9], own[1][5:9] = 0.0, float("nan"), float("nan")
+    Q = torch.randn(n_pre * fan, g, 1, d, generator=gen, device="cuda").to(dtype)
+    p = bk.make_params(d, 64, 1, dtype, log_c=0.0)
+    out, lse = bk.attend_prefix(p, pre, own, Q, count_own=cs)
+    alone, lse2 = bk.attend_prefix(p, pre, own, Q, count_prefix=0, count_own=cs)
+    for s in list(range(12)) + [100, 301, 302]:
+        K, V, w = (torch.cat([a[s % n_pre], b[s, :cs]]) for a, b in zip(pre, own))
+        _check_out(out[s], lse[s], _attention(Q[s].reshape(-1, d), K, V, w), dtype, cp + cs, "sequence %d" % s, fan * g)
+        _check_out(alone[s], lse2[s], _attention(Q[s].reshape(-1, d), own[0][s, :cs], own[1][s, :cs], own[2][s, :cs]), dtype, cs, "sequence %d alone" % s)
