@@ -529,7 +529,8 @@ int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const
         a.set[0].stride = stride_tokens; a.set[0].count = count;
         a.Q = (const char*)Q; a.out = (char*)out; a.lse_out = lse_out; a.n_seq = n_seq; a.n_q = n_q;
         a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)p->d));
-        const hipError_t e = bkv::launch_attend_mass(p->dtype, p->d, a, bkv::AttendMass{mass_in, mass_out, decay}, workspace, st);
+        a.mass = mass_in; a.mass_out = mass_out; a.decay = decay;
+        const hipError_t e = bkv::launch_attend_mass(p->dtype, p->d, a, workspace, st);
         return e == hipSuccess ? BKV_OK : hip_fail(e);
     }
     // rows of a cache in the order of their positions, its query heads next to each other

@@ -174,14 +174,47 @@ __device__ __forceinline__ void merge_rows(const float* part, size_t sstride, in
     }
 }
 
+// Masses of the four places from `key` on: mass_out = decay mass + sum_q 2^(logit - m_q) / l_q, ml[q] = {m_q, 1 / l_q}.  Groups without
+// a token have no logits: what is there is not looked at.
+__device__ __forceinline__ void store_masses(const AttendArgs& a, size_t seq0, int64_t key, const float* logits, const floatx2* ml) {
+    const AttendSet& S = a.set[0];
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int q = 0; q < a.n_q; ++q) {
+        const floatx4 x = *reinterpret_cast<const floatx4*>(logits + q * 16);
+        const floatx2 st = ml[q];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(fast_exp2(x[e] - st[0]), st[1], acc[e]);
+    }
+    const size_t at = seq0 + key;
+    if (key + 4 <= S.count) {
+        const floatx4_u w = *reinterpret_cast<const floatx4_u*>(S.w + at);
+        floatx4_u old = {0.f, 0.f, 0.f, 0.f}, out;
+        if (a.mass) old = *reinterpret_cast<const floatx4_u*>(a.mass + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float x = w[e] > 0.f ? acc[e] : 0.f;
+            out[e] = a.mass ? fmaf(a.decay, old[e], x) : x;
+        }
+        *reinterpret_cast<floatx4_u*>(a.mass_out + at) = out;
+    } else {
+        for (int e = 0; key + e < S.count; ++e) {
+            const float x = S.w[at + e] > 0.f ? acc[e] : 0.f;
+            a.mass_out[at + e] = a.mass ? fmaf(a.decay, a.mass[at + e], x) : x;
+        }
+    }
+}
+
 // One workgroup of W wavefronts: NQT x 16 queries of one sequence against one range of keys; its wavefronts take the
 // key groups of the range in turn.  Registers (NQT = 1, bf16, d = 128): 64 for the K and V rows in flight, 16 queries, 32
 // sums.  The rows of the next group are requested as soon as the registers of the current one are free (keys after S^T,
 // values after O^T), so that about 12 KB per wavefront are under way at any time.
 // STREAM: K and V are read past the caches (see attend_streams).
 // ONE: a workgroup takes both sets of a sequence as a whole, nothing is merged behind it (see attend_in_one).
-// LOGITS: the logits of every group that holds a token go to memory, value rows of absent tokens count as zeros whatever they hold.
-template <typename T, int D, int NQT, int W, bool STREAM = false, bool ONE = false, bool LOGITS = false>
+// LOGITS: the logits of every group that holds a token are kept, value rows of absent tokens count as zeros whatever they hold.
+// kLogitsOut: in memory, for attend_mass_kernel.  kLogitsHeld: in LDS, the workgroup has a whole sequence and sums its tokens' masses itself.
+constexpr int kLogitsOut = 1, kLogitsHeld = 2;
+template <typename T, int D, int NQT, int W, bool STREAM = false, bool ONE = false, int LOGITS = 0>
 __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
     constexpr bool B16 = sizeof(T) == 2;
     constexpr int ROWB = D * (int)sizeof(T);
@@ -194,8 +227,15 @@ __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
     constexpr int RQ = 16 * NQT;
     constexpr int P = D + kRowPad;
 
-    // the wavefronts' sums meet here
-    __shared__ __align__(16) float lds[W * RQ * P];
+    // the wavefronts' sums meet here (LDS of the launch, held logits: rows of the queries that there are, reference exponents and
+    // 1 / denominators behind them, then the logits as kLogitsOut has them)
+    constexpr bool HELD = LOGITS == kLogitsHeld;
+    __shared__ __align__(16) float lds_own[HELD ? 1 : W * RQ * P];
+    extern __shared__ __align__(16) float lds_held[];
+    float* const lds = HELD ? lds_held : lds_own;
+    const int meet = HELD ? a.n_q * P : RQ * P;                  // a wavefront's
+    float* const held_stats = lds_held + W * meet;
+    float* const held = held_stats + 32;
     __shared__ int last_flag;
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -436,16 +476,16 @@ __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
             for (int t = 0; t < NQT; ++t)
 #pragma unroll
                 for (int x = 0; x < VR; ++x) s[t][x >> 2][x & 3] = w[x] > 0.f ? s[t][x >> 2][x & 3] : 0.f;
-            if constexpr (LOGITS) {
+            if constexpr (LOGITS != 0) {
 #pragma unroll
                 for (int x = 0; x < VR; ++x)
 #pragma unroll
                     for (int c = 0; c < VD; ++c) vf[x][c] = w[x] > 0.f ? vf[x][c] : 0u;
             }
         }
-        if constexpr (LOGITS) {
+        if constexpr (LOGITS != 0) {
             if (n < a.n_q) {
-                float* to = a.logits + ((((size_t)seq * groups + group) * NT) * a.n_q + n) * 16 + 4 * kg;
+                float* to = (HELD ? held + ((int)group * NT * a.n_q + n) * 16 : a.logits + ((((size_t)seq * groups + group) * NT) * a.n_q + n) * 16) + 4 * kg;
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     floatx4 x;
@@ -592,7 +632,7 @@ __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
 #pragma unroll
     for (int t = 0; t < NQT; ++t)
         if (16 * t + n < nqv) {
-            float* row = lds + (wave * RQ + 16 * t + n) * P;
+            float* row = lds + wave * meet + (16 * t + n) * P;
             if (has_v) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
@@ -636,18 +676,20 @@ __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
         floatx2 ml[W];
         float M = kNeg, L = 0.f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) { ml[w] = *reinterpret_cast<const floatx2*>(row + w * RQ * P + D); M = fmaxf(M, ml[w][0]); }
+        for (int w = 0; w < W; ++w) { ml[w] = *reinterpret_cast<const floatx2*>(row + w * meet + D); M = fmaxf(M, ml[w][0]); }
         floatx4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             const float f = fast_exp2(ml[w][0] - M);
             L = fmaf(ml[w][1], f, L);
-            if (has_v) acc += *reinterpret_cast<const floatx4*>(row + w * RQ * P + col) * f;
+            if (has_v) acc += *reinterpret_cast<const floatx4*>(row + w * meet + col) * f;
         }
         if (ns == 1) {                          // the whole range was one split: normalise and store
             store4<T>(a.out, (row0 + q) * D + col, acc * (L > 0.f ? 1.f / L : 0.f));
             if (col == 0 && a.lse_out) a.lse_out[row0 + q] = L > 0.f ? log2_or(L, M) * 0.6931471805599453f : -INFINITY;
-            if constexpr (LOGITS) {
+            if constexpr (HELD) {
+                if (col == 0) *reinterpret_cast<floatx2*>(held_stats + 2 * q) = floatx2{M, L > 0.f ? 1.f / L : 0.f};
+            } else if constexpr (LOGITS == kLogitsOut) {
                 if (col == 0) *reinterpret_cast<floatx2*>(a.stats + 2 * (row0 + q)) = floatx2{M, L > 0.f ? 1.f / L : 0.f};
             }
         } else {
@@ -655,6 +697,12 @@ __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
             if (has_v) { put2(dst + col, acc[0], acc[1]); put2(dst + col + 2, acc[2], acc[3]); }
             if (col == 0) put2(dst + D, M, L);
         }
+    }
+    if constexpr (HELD) {
+        __syncthreads();
+        for (int64_t key = 4 * tid; key < S.count; key += 4 * W * 64)
+            store_masses(a, (size_t)seq * S.stride, key, held + ((int)(key / 16) * a.n_q) * 16 + key % 16, reinterpret_cast<const floatx2*>(held_stats));
+        return;
     }
     if (ONE || ns == 1 || !a.fused) return;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // this wavefront's share of the partial has reached memory ...
@@ -685,7 +733,7 @@ __global__ __launch_bounds__(kMergeThreads) void attend_merge_kernel(const Atten
 // the others has 1024 places of a sequence, mass_out = decay mass + sum_q 2^(logit - m_q) / l_q.  It puts m and l of the sequence's
 // queries together from the partial rows by itself, so that one launch does both.
 template <typename T, int D>
-__global__ __launch_bounds__(kMergeThreads) void attend_mass_kernel(const AttendArgs a, const AttendMass b, uint32_t merge_blocks) {
+__global__ __launch_bounds__(kMergeThreads) void attend_mass_kernel(const AttendArgs a, uint32_t merge_blocks) {
     constexpr int P = D + kRowPad, KEYS = sizeof(T) == 2 ? 32 : 16;
     __shared__ __align__(16) float red[kMergeThreads * 8];
     uint32_t block = blockIdx.y * gridDim.x + blockIdx.x;
@@ -725,32 +773,7 @@ __global__ __launch_bounds__(kMergeThreads) void attend_mass_kernel(const Attend
     const int64_t key = 4 * ((int64_t)(block % chunks) * kMergeThreads + threadIdx.x);
     if (key >= S.count) return;
     const float* lg = a.logits + ((size_t)seq * ((S.count + KEYS - 1) / KEYS * (KEYS / 16)) + key / 16) * a.n_q * 16 + key % 16;
-    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int q = 0; q < a.n_q; ++q) {
-        const floatx4 x = *reinterpret_cast<const floatx4*>(lg + q * 16);
-        const floatx2 ml = st[q];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = fmaf(fast_exp2(x[e] - ml[0]), ml[1], acc[e]);
-    }
-    // (groups without a token have not been written: what is there is not looked at)
-    const size_t at = (size_t)seq * S.stride + key;
-    if (key + 4 <= S.count) {
-        const floatx4_u w = *reinterpret_cast<const floatx4_u*>(S.w + at);
-        floatx4_u old = {0.f, 0.f, 0.f, 0.f}, out;
-        if (b.mass) old = *reinterpret_cast<const floatx4_u*>(b.mass + at);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float x = w[e] > 0.f ? acc[e] : 0.f;
-            out[e] = b.mass ? fmaf(b.decay, old[e], x) : x;
-        }
-        *reinterpret_cast<floatx4_u*>(b.mass_out + at) = out;
-    } else {
-        for (int e = 0; key + e < S.count; ++e) {
-            const float x = S.w[at + e] > 0.f ? acc[e] : 0.f;
-            b.mass_out[at + e] = b.mass ? fmaf(b.decay, b.mass[at + e], x) : x;
-        }
-    }
+    store_masses(a, (size_t)seq * S.stride, key, lg, st);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -882,26 +905,50 @@ size_t attend_mass_bytes(int dtype, int d, int64_t n_seq, int64_t count, int n_q
     return mass_align(logit_bytes(dtype, n_seq, count, n_q)) + mass_align((size_t)n_seq * n_q * 8) + mass_align(attend_workspace_bytes(d, n_seq, n_q, 1));
 }
 
+// Bytes of LDS for the logits of a whole sequence beside the wavefronts' sums, 0 where the splits are taken: a workgroup per sequence is one
+// launch, and its writes are the masses alone (among 2.2 GB read, 68 MB of logits cost 110 us, wherever they go in memory).  Taken where
+// sequences are enough for the compute units, or so short (a few steps of eight wavefronts) that splitting them buys less than the second
+// launch costs.  Held / split, 4 queries, us a call: bf16, d = 128, 512 x 8300 tokens 355 / 463, 256 x 8300 172 / 232, 200 x 2000 33 / 43,
+// 300 x 8300 293 / 301 (a second round of 44), 128 x 8300 141 / 116, 64 x 512 11.8 / 14.5, 64 x 1024 16.5 / 14.7; d = 64, 512 x 8300 191 / 255,
+// 64 x 1024 12.3 / 14.0; fp32, d = 128, 256 x 8300 344 / 434, 64 x 256 13.0 / 14.2, 64 x 384 16.2 / 14.9.
+constexpr int kHeldWaves = 8;
+constexpr size_t kHeldMost = 160 * 1024 - 256;
+static size_t held_bytes(int row_bytes, int d, int keys, const AttendArgs& a) {
+    const int64_t count = a.set[0].count, n_cu = compute_units(), rounds = n_cu > 0 ? (a.n_seq + n_cu - 1) / n_cu : 0;
+    const bool fills = rounds > 0 && 8 * a.n_seq >= 5 * rounds * n_cu, is_short = 2 * count * row_bytes <= 256 * 1024;
+    const size_t bytes = ((size_t)kHeldWaves * a.n_q * (d + kRowPad) + 32 + (size_t)a.n_q * ((count + keys - 1) / keys * keys)) * sizeof(float);
+    return (fills || is_short) && bytes <= kHeldMost ? bytes : 0;
+}
+
 template <typename T, int D>
-static hipError_t launch_attend_mass_t(const AttendArgs& a, const AttendMass& b, const AttendPlan& p, hipStream_t st) {
+static hipError_t launch_attend_mass_t(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
     const dim3 grid((unsigned int)p.ns[0], (unsigned)a.n_seq);
     const int64_t units = a.n_seq * a.set[0].count;
     hipError_t e = hipSuccess;
-    if (attend_streams(D * (int)sizeof(T), a)) {
-        if (p.waves == 8) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 8, true, false, true>, grid, dim3(512), 0, st, a);
-        else if constexpr (sizeof(T) == 2) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 4, true, false, true>, grid, dim3(256), 0, st, a);
-    } else if (p.waves == 8) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 8, false, false, true>, grid, dim3(512), 0, st, a);
-    else if constexpr (sizeof(T) == 2) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 4, false, false, true>, grid, dim3(256), 0, st, a);
+    const bool past = attend_streams(D * (int)sizeof(T), a);
+    if (const size_t held = held_bytes(D * (int)sizeof(T), D, sizeof(T) == 2 ? 32 : 16, a); held > 0) {
+        AttendArgs one = a;
+        one.ns[0] = 1; one.set[0].groups_per_split = (int32_t)((a.set[0].count + 15) / 16);
+        auto kern = past ? attend_kernel<T, D, 1, kHeldWaves, true, false, kLogitsHeld> : attend_kernel<T, D, 1, kHeldWaves, false, false, kLogitsHeld>;
+        if (held > 64 * 1024) e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)held);
+        if (e != hipSuccess) return e;
+        return launch_timed(kProfAttend, units, kern, dim3(1, (unsigned)a.n_seq), dim3(64 * kHeldWaves), held, st, one);
+    }
+    if (past) {
+        if (p.waves == 8) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 8, true, false, kLogitsOut>, grid, dim3(512), 0, st, a);
+        else if constexpr (sizeof(T) == 2) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 4, true, false, kLogitsOut>, grid, dim3(256), 0, st, a);
+    } else if (p.waves == 8) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 8, false, false, kLogitsOut>, grid, dim3(512), 0, st, a);
+    else if constexpr (sizeof(T) == 2) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 4, false, false, kLogitsOut>, grid, dim3(256), 0, st, a);
     if (e != hipSuccess) return e;
     const uint64_t merges = p.ns[0] > 1 ? (uint64_t)a.n_seq * a.n_q : 0;
     const uint64_t all = merges + (uint64_t)a.n_seq * ((a.set[0].count + 4 * kMergeThreads - 1) / (4 * kMergeThreads));
     if (all >= (uint64_t)1 << 31) return hipErrorInvalidValue;
     const uint32_t gx = all > 65536 ? 65536u : (uint32_t)all;
-    return launch_timed(kProfAttendMerge, a.n_seq * a.n_q, attend_mass_kernel<T, D>, dim3(gx, (uint32_t)((all + gx - 1) / gx)), dim3(kMergeThreads), 0, st, a, b,
+    return launch_timed(kProfAttendMerge, a.n_seq * a.n_q, attend_mass_kernel<T, D>, dim3(gx, (uint32_t)((all + gx - 1) / gx)), dim3(kMergeThreads), 0, st, a,
                         (uint32_t)merges);
 }
 
-hipError_t launch_attend_mass(int dtype, int d, AttendArgs& a, const AttendMass& b, void* workspace, hipStream_t st) {
+hipError_t launch_attend_mass(int dtype, int d, AttendArgs& a, void* workspace, hipStream_t st) {
     if (a.n_q > 16 || a.set[0].count <= 0 || a.set[1].count != 0) return hipErrorInvalidValue;
     const AttendPlan p = attend_plan(d, dtype == BKV_BF16 ? 2 : 4, a.n_seq, a.set[0].count, 0, a.n_q, kAttendPartialBytes);
     a.n_qg = p.n_qg; a.rows = p.rows; a.fused = 0; a.by_xcd = 0;
@@ -911,10 +958,10 @@ hipError_t launch_attend_mass(int dtype, int d, AttendArgs& a, const AttendMass&
     ws += mass_align(logit_bytes(dtype, a.n_seq, a.set[0].count, a.n_q));
     a.stats = (float*)ws;
     a.partial = (float*)(ws + mass_align((size_t)a.n_seq * a.n_q * 8));
-    if (dtype == BKV_BF16 && d == 128) return launch_attend_mass_t<__bf16, 128>(a, b, p, st);
-    if (dtype == BKV_BF16 && d == 64) return launch_attend_mass_t<__bf16, 64>(a, b, p, st);
-    if (dtype == BKV_F32 && d == 128) return launch_attend_mass_t<float, 128>(a, b, p, st);
-    if (dtype == BKV_F32 && d == 64) return launch_attend_mass_t<float, 64>(a, b, p, st);
+    if (dtype == BKV_BF16 && d == 128) return launch_attend_mass_t<__bf16, 128>(a, p, st);
+    if (dtype == BKV_BF16 && d == 64) return launch_attend_mass_t<__bf16, 64>(a, p, st);
+    if (dtype == BKV_F32 && d == 128) return launch_attend_mass_t<float, 128>(a, p, st);
+    if (dtype == BKV_F32 && d == 64) return launch_attend_mass_t<float, 64>(a, p, st);
     return hipErrorInvalidValue;
 }
 

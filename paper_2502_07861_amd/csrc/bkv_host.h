@@ -212,19 +212,17 @@ struct AttendArgs {
     // launch_attend_mass alone
     float* logits;            // [n_seq, tiles of 16 keys, n_q, 16]: log2 of w_j e^{<k_j,q>/sqrt d}
     float* stats;             // [n_seq, n_q, 2]: reference exponent and 1 / denominator, where the range is one split
-};
-// Workspace bound for any count; `sets`: 1, or 2 when numerator and denominator run over sets of their own.
-size_t attend_workspace_bytes(int d, int64_t n_seq, int n_q, int sets = 1);
-// The same pass over one set with its logits kept, and from them mass_out[j] = decay mass[j] + sum over the queries of their weight on
-// token j: one launch more, which also merges the splits.
-struct AttendMass {
     const float* mass;        // [n_seq, set stride] or null (zeros)
     float* mass_out;
     float decay;
 };
+// Workspace bound for any count; `sets`: 1, or 2 when numerator and denominator run over sets of their own.
+size_t attend_workspace_bytes(int d, int64_t n_seq, int n_q, int sets = 1);
+// The same pass over one set with its logits kept, and from them mass_out[j] = decay mass[j] + sum over the queries of their weight on
+// token j: in the same launch where they stay in LDS, else in one more, which also merges the splits.
 bool attend_keeps_logits(int row_bytes, int64_t n_q);     // are they fewer bytes than reading the keys a second time?
 size_t attend_mass_bytes(int dtype, int d, int64_t n_seq, int64_t count, int n_q);
-hipError_t launch_attend_mass(int dtype, int d, AttendArgs& a, const AttendMass& b, void* workspace, hipStream_t st);
+hipError_t launch_attend_mass(int dtype, int d, AttendArgs& a, void* workspace, hipStream_t st);
 // max_bytes: what the partial rows may take (fewer splits where they would take more)
 hipError_t launch_attend(int dtype, int d, AttendArgs& a, void* workspace, size_t ws_bytes, size_t max_bytes, hipStream_t st);
 // the entry point without allocations: what a launch of this shape writes into the scratch buffer, and the

@@ -143,6 +143,9 @@ MASS = [  # dtype, d, n_seq, count, g, nq, visible, decay
     (F32, 64, 3, 4097, 4, 1, None, 1.0), (F32, 128, 2, 500, 1, 130, 371, 0.9), (F32, 64, 1, 70, 7, 70, 1, 1.0), (BF16, 128, 2, 500, 2, 10, -1000, 1.0),
     (BF16, 128, 2, 40, 2, 90, 1, 1.0), (BF16, 128, 9, 250, 3, 250, 1, 1.0), (BF16, 64, 50, 140, 2, 70, 71, 0.5), (F32, 128, 9, 150, 2, 100, 51, 1.0),
     (BF16, 128, 3, 2000, 1, 500, 1501, 1.0), (BF16, 64, 1, 640, 8, 640, -3, 0.0),
+    (BF16, 128, 161, 2001, 4, 1, None, 0.5), (BF16, 64, 330, 77, 4, 2, None, 1.0), (F32, 128, 170, 777, 16, 1, None, 0.0), (F32, 64, 165, 1001, 1, 1, None, 1.0),
+    (BF16, 128, 160, 8768, 4, 1, None, 1.0), (BF16, 128, 160, 9100, 4, 1, None, 1.0), (BF16, 128, 600, 1, 3, 1, None, 1.0), (BF16, 128, 5, 513, 2, 1, None, 1.0),
+    (BF16, 128, 5, 512, 2, 8, None, 1.0), (F32, 128, 5, 256, 5, 3, None, 1.0), (F32, 128, 5, 257, 5, 3, None, 1.0), (BF16, 64, 5, 1024, 1, 7, None, 1.0),
 ]
 
 
