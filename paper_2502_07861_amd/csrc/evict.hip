@@ -126,12 +126,60 @@ __device__ __forceinline__ void end_list(const EvictArgs& a, int64_t seq, int2 t
     if (threadIdx.x == 0 && a.count_out) a.count_out[seq] = n;
 }
 
+// Rows to their places: 16 bytes of keys and of values a lane and step, kGatherSteps of them on their way; piece `first` and every
+// `step`-th after it.
+constexpr int kGatherSteps = 4;
+template <int SLOTS, int THREADS>
+__device__ __forceinline__ void gather_rows(const EvictArgs& a, int64_t seq, int first, int step) {
+    constexpr int RPS = THREADS / SLOTS;                             // rows of a step
+    const int32_t* pick = a.pick + (size_t)seq * a.keep;
+    const size_t in = (size_t)seq * a.stride, out = (size_t)seq * a.keep;
+    const int slot = threadIdx.x % SLOTS, r0 = threadIdx.x / SLOTS;
+    for (int64_t base = (int64_t)first * (RPS * kGatherSteps); base < a.keep; base += (int64_t)step * (RPS * kGatherSteps)) {
+        int p[kGatherSteps];
+        uintx4 k[kGatherSteps], v[kGatherSteps];
+#pragma unroll
+        for (int i = 0; i < kGatherSteps; ++i) {
+            const int r = (int)base + RPS * i + r0;
+            p[i] = pick[min(r, a.keep - 1)];
+        }
+#pragma unroll
+        for (int i = 0; i < kGatherSteps; ++i) {
+            const size_t from = (in + (size_t)max(p[i], 0)) * (SLOTS * 16) + slot * 16;
+            k[i] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(a.K + from));
+            v[i] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(a.V + from));
+        }
+#pragma unroll
+        for (int i = 0; i < kGatherSteps; ++i) {
+            const int r = (int)base + RPS * i + r0;
+            if (r >= a.keep) break;
+            const size_t to = (out + r) * (SLOTS * 16) + slot * 16;
+            if (p[i] < 0) { k[i] = uintx4{0u, 0u, 0u, 0u}; v[i] = k[i]; }
+            __builtin_nontemporal_store(k[i], reinterpret_cast<uintx4*>(a.K_out + to));
+            __builtin_nontemporal_store(v[i], reinterpret_cast<uintx4*>(a.V_out + to));
+        }
+        const int r = (int)base + (int)threadIdx.x;
+        if (threadIdx.x < RPS * kGatherSteps && r < a.keep) {
+            const int at = pick[r];
+            if (a.w_out) a.w_out[out + r] = at >= 0 ? a.w[in + at] : 0.f;
+            if (a.mass_out) a.mass_out[out + r] = at >= 0 ? a.mass[in + at] : 0.f;
+            if (a.idx_out) a.idx_out[out + r] = at < 0 ? -1 : a.idx ? a.idx[in + at] : at;
+        }
+    }
+}
+
+template <int SLOTS>
+__global__ __launch_bounds__(kGatherThreads) void evict_gather_kernel(const EvictArgs a) {
+    gather_rows<SLOTS, kGatherThreads>(a, blockIdx.y, blockIdx.x, gridDim.x);
+}
+
 // A workgroup a sequence, KPT ranks a thread in registers.  The keep-th largest rank is found seven bits at a time from counts of
 // 128 bins, every lane with counters of its own (masses share their upper bits: bins that lanes share are all hit at once, 81 us for
 // 8 x 16384 places in all; bit by bit by ballots of all ranks 19), until few ranks are left that it can be, mostly after two steps;
 // those one wavefront searches bit by bit.
+// SLOTS: it moves the rows, of so many 16-byte slots, as well; 0: a launch behind this one does.
 constexpr int kFew = 512, kDigit = 7, kBins = 1 << kDigit;
-template <int KPT>
+template <int KPT, int SLOTS = 0>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const EvictArgs a) {
     __shared__ __align__(16) unsigned int bins[2][kBins * 64];
     __shared__ __align__(16) unsigned int sums[kBins];
@@ -211,6 +259,10 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
     sum_ranks<KPT>(x, cut, make_int2(0, 0), waves, before, total);
     list_ranks<KPT>(x, cut, 0, a.pick + (size_t)seq * a.keep, before);
     end_list(a, seq, total, cut);
+    if constexpr (SLOTS > 0) {
+        __syncthreads();
+        gather_rows<SLOTS, kSelectThreads>(a, seq, 0, 1);
+    }
 }
 
 // Longer sequences: a workgroup per 8192 places (few enough that places of one bin do not hold each other up for long), the same
@@ -305,48 +357,6 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(const EvictA
     if (blockIdx.x + 1 == gridDim.x) end_list(a, seq, total, cut);
 }
 
-// Rows to their places: 16 bytes of keys and of values a lane and step, kGatherSteps of them on their way.
-constexpr int kGatherSteps = 4;
-template <int SLOTS>
-__global__ __launch_bounds__(kGatherThreads) void evict_gather_kernel(const EvictArgs a) {
-    constexpr int RPS = kGatherThreads / SLOTS;                      // rows of a step
-    const int64_t seq = blockIdx.y;
-    const int32_t* pick = a.pick + (size_t)seq * a.keep;
-    const size_t in = (size_t)seq * a.stride, out = (size_t)seq * a.keep;
-    const int slot = threadIdx.x % SLOTS, r0 = threadIdx.x / SLOTS;
-    for (int base = blockIdx.x * (RPS * kGatherSteps); base < a.keep; base += gridDim.x * (RPS * kGatherSteps)) {
-        int p[kGatherSteps];
-        uintx4 k[kGatherSteps], v[kGatherSteps];
-#pragma unroll
-        for (int i = 0; i < kGatherSteps; ++i) {
-            const int r = base + RPS * i + r0;
-            p[i] = pick[min(r, a.keep - 1)];
-        }
-#pragma unroll
-        for (int i = 0; i < kGatherSteps; ++i) {
-            const size_t from = (in + (size_t)max(p[i], 0)) * (SLOTS * 16) + slot * 16;
-            k[i] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(a.K + from));
-            v[i] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(a.V + from));
-        }
-#pragma unroll
-        for (int i = 0; i < kGatherSteps; ++i) {
-            const int r = base + RPS * i + r0;
-            if (r >= a.keep) break;
-            const size_t to = (out + r) * (SLOTS * 16) + slot * 16;
-            if (p[i] < 0) { k[i] = uintx4{0u, 0u, 0u, 0u}; v[i] = k[i]; }
-            __builtin_nontemporal_store(k[i], reinterpret_cast<uintx4*>(a.K_out + to));
-            __builtin_nontemporal_store(v[i], reinterpret_cast<uintx4*>(a.V_out + to));
-        }
-        const int r = base + (int)threadIdx.x;
-        if (threadIdx.x < RPS * kGatherSteps && r < a.keep) {
-            const int at = pick[r];
-            if (a.w_out) a.w_out[out + r] = at >= 0 ? a.w[in + at] : 0.f;
-            if (a.mass_out) a.mass_out[out + r] = at >= 0 ? a.mass[in + at] : 0.f;
-            if (a.idx_out) a.idx_out[out + r] = at < 0 ? -1 : a.idx ? a.idx[in + at] : at;
-        }
-    }
-}
-
 constexpr int kOnePlaces = 64 * kSelectThreads;            // places whose ranks fit the registers of one workgroup
 
 static size_t list_bytes(int64_t n_seq, int64_t count) { return ((size_t)n_seq * count * sizeof(int32_t) + 255) / 256 * 256; }
@@ -378,12 +388,28 @@ static hipError_t launch_long(const EvictArgs& a, hipStream_t st) {
     return e;
 }
 
+template <int SLOTS>
+static hipError_t launch_whole(const EvictArgs& a, hipStream_t st) {
+    const dim3 grid((uint32_t)a.n_seq), block(kSelectThreads);
+    if (a.count <= 4 * kSelectThreads) hipLaunchKernelGGL((evict_select_kernel<4, SLOTS>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((evict_select_kernel<16, SLOTS>), grid, block, 0, st, a);
+    return hipGetLastError();
+}
+
 hipError_t launch_evict(EvictArgs& a, void* workspace, hipStream_t st) {
     a.pick = (int32_t*)workspace;
     a.hist = (unsigned int*)((char*)workspace + list_bytes(a.n_seq, a.count));
     a.chunk = (int2*)((char*)a.hist + hist_bytes(a.n_seq));
     const dim3 grid((uint32_t)a.n_seq), block(kSelectThreads);
     hipError_t e = hipSuccess;
+    // Few rows: the workgroup that chose them moves them, one launch.  One compute unit copies slower than the launch of many takes from
+    // here on.  Both sides, us a call, 8 sequences / the same in a captured graph / 256 sequences: 50 KB kept 8.5 for 11.9 / 8.5 for 8.7 / 12.1 for 14.3,
+    // 128 KB (of 4000 places) 9.6 for 12.6 / 9.6 for 9.7 / 19.2 for 22.3, 256 KB 12.0 for 12.7 / 12.1 for 9.7 / 31.6 for 34.2, 500 KB 16.8 for 13.0.
+    if (a.count <= 16 * kSelectThreads && (int64_t)2 * a.keep * a.row_bytes <= 192 * 1024) {
+        if (a.row_bytes == 128) return launch_whole<8>(a, st);
+        if (a.row_bytes == 256) return launch_whole<16>(a, st);
+        return launch_whole<32>(a, st);
+    }
     if (a.count > kOnePlaces) e = launch_long(a, st);
     else {
         if (a.count <= 4 * kSelectThreads) hipLaunchKernelGGL(evict_select_kernel<4>, grid, block, 0, st, a);

@@ -252,7 +252,8 @@ EVICT = [  # dtype, d, n_seq, count, extra stride, keep, sink, recent
     (BF16, 128, 1, 1, 0, 1, 0, 0), (BF16, 128, 3, 100, 7, 40, 4, 8), (BF16, 64, 2, 1025, 0, 512, 0, 100), (BF16, 128, 2, 5000, 3, 4999, 1, 1),
     (BF16, 128, 2, 5000, 3, 1, 0, 0), (BF16, 128, 2, 5000, 0, 1, 1, 0), (BF16, 64, 5, 4096, 0, 4096, 10, 10), (BF16, 128, 2, 20000, 0, 3000, 256, 256),
     (BF16, 64, 1, 70001, 0, 20000, 4, 100), (BF16, 64, 1, 300000, 5, 100001, 4, 100), (F32, 128, 2, 777, 1, 300, 0, 300), (F32, 64, 4, 1111, 9, 301, 3, 17), (F32, 64, 300, 65, 0, 31, 1, 1),
-    (F32, 128, 1, 33000, 0, 8000, 8, 8),
+    (F32, 128, 1, 33000, 0, 8000, 8, 8), (BF16, 128, 2, 16384, 0, 384, 0, 5), (BF16, 128, 2, 16385, 1, 384, 4, 5), (BF16, 64, 3, 9000, 2, 768, 1, 1),
+    (F32, 128, 2, 600, 0, 193, 1, 1),
 ]
 
 
