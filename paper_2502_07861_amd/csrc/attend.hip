@@ -905,19 +905,25 @@ size_t attend_mass_bytes(int dtype, int d, int64_t n_seq, int64_t count, int n_q
     return mass_align(logit_bytes(dtype, n_seq, count, n_q)) + mass_align((size_t)n_seq * n_q * 8) + mass_align(attend_workspace_bytes(d, n_seq, n_q, 1));
 }
 
-// Bytes of LDS for the logits of a whole sequence beside the wavefronts' sums, 0 where the splits are taken: a workgroup per sequence is one
-// launch, and its writes are the masses alone (among 2.2 GB read, 68 MB of logits cost 110 us, wherever they go in memory).  Taken where
-// sequences are enough for the compute units, or so short (a few steps of eight wavefronts) that splitting them buys less than the second
-// launch costs.  Held / split, 4 queries, us a call: bf16, d = 128, 512 x 8300 tokens 355 / 463, 256 x 8300 172 / 232, 200 x 2000 33 / 43,
-// 300 x 8300 293 / 301 (a second round of 44), 128 x 8300 141 / 116, 64 x 512 11.8 / 14.5, 64 x 1024 16.5 / 14.7; d = 64, 512 x 8300 191 / 255,
-// 64 x 1024 12.3 / 14.0; fp32, d = 128, 256 x 8300 344 / 434, 64 x 256 13.0 / 14.2, 64 x 384 16.2 / 14.9.
-constexpr int kHeldWaves = 8;
-constexpr size_t kHeldMost = 160 * 1024 - 256;
-static size_t held_bytes(int row_bytes, int d, int keys, const AttendArgs& a) {
-    const int64_t count = a.set[0].count, n_cu = compute_units(), rounds = n_cu > 0 ? (a.n_seq + n_cu - 1) / n_cu : 0;
-    const bool fills = rounds > 0 && 8 * a.n_seq >= 5 * rounds * n_cu, is_short = 2 * count * row_bytes <= 256 * 1024;
-    const size_t bytes = ((size_t)kHeldWaves * a.n_q * (d + kRowPad) + 32 + (size_t)a.n_q * ((count + keys - 1) / keys * keys)) * sizeof(float);
-    return (fills || is_short) && bytes <= kHeldMost ? bytes : 0;
+// A workgroup for a whole sequence holds its logits in LDS beside the wavefronts' sums: one launch, and its writes are the masses alone (among
+// 2.2 GB read, 68 MB of logits cost 110 us, wherever they go in memory).  Taken where the compute units get equal shares of the sequences, or
+// these are so short (a few steps of eight wavefronts) that splitting them buys less than the second launch costs.  Held / split, 4 queries, us a
+// call: bf16, d = 128, 512 x 8300 tokens 355 / 463, 256 x 8300 172 / 232, 200 x 2000 33 / 43, 260 x 8300 with shares of 2 and 1 as long as with splits,
+// 128 x 8300 141 / 116, 64 x 512 11.8 / 14.5, 64 x 1024 16.5 / 14.7; d = 64, 512 x 8300 191 / 255, 64 x 1024 12.3 / 14.0; fp32, d = 128,
+// 256 x 8300 344 / 434, 64 x 256 13.0 / 14.2, 64 x 384 16.2 / 14.9.
+// Four wavefronts (bf16) where sequences are more than compute units and two or more have room in one: one starts while another ends.  Four / eight /
+// split: 1024 x 250 25.4 / 34.3 / 28.1, 512 x 2000 84 / 90 / 108, 9000 x 100 111 / 187 / 122.
+constexpr size_t kHeldMost = 160 * 1024 - 256, kHeldTwo = 80 * 1024;
+static size_t held_bytes(int d, int keys, int waves, const AttendArgs& a) {
+    return ((size_t)waves * a.n_q * (d + kRowPad) + 32 + (size_t)a.n_q * ((a.set[0].count + keys - 1) / keys * keys)) * sizeof(float);
+}
+// wavefronts of such a workgroup, 0: splits
+static int held_waves(int row_bytes, int d, int keys, int waves, const AttendArgs& a) {
+    const int64_t n_cu = compute_units(), rounds = n_cu > 0 ? (a.n_seq + n_cu - 1) / n_cu : 0;
+    const bool fills = rounds > 0 && 16 * a.n_seq >= 11 * rounds * n_cu, is_short = 2 * a.set[0].count * row_bytes <= 256 * 1024;
+    if (!fills && !is_short) return 0;
+    if (waves == 4 && rounds > 1 && held_bytes(d, keys, 4, a) <= kHeldTwo) return 4;
+    return held_bytes(d, keys, 8, a) <= kHeldMost ? 8 : 0;
 }
 
 template <typename T, int D>
@@ -926,14 +932,19 @@ static hipError_t launch_attend_mass_t(const AttendArgs& a, const AttendPlan& p,
     const int64_t units = a.n_seq * a.set[0].count;
     hipError_t e = hipSuccess;
     const bool past = attend_streams(D * (int)sizeof(T), a);
-    if (const size_t held = held_bytes(D * (int)sizeof(T), D, sizeof(T) == 2 ? 32 : 16, a); held > 0) {
+    auto whole = [&](auto waves) {                                       // a workgroup a sequence
+        constexpr int W = decltype(waves)::value;
         AttendArgs one = a;
         one.ns[0] = 1; one.set[0].groups_per_split = (int32_t)((a.set[0].count + 15) / 16);
-        auto kern = past ? attend_kernel<T, D, 1, kHeldWaves, true, false, kLogitsHeld> : attend_kernel<T, D, 1, kHeldWaves, false, false, kLogitsHeld>;
-        if (held > 64 * 1024) e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)held);
+        const size_t lds = held_bytes(D, sizeof(T) == 2 ? 32 : 16, W, a);
+        auto kern = past ? attend_kernel<T, D, 1, W, true, false, kLogitsHeld> : attend_kernel<T, D, 1, W, false, false, kLogitsHeld>;
+        if (lds > 64 * 1024) e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
-        return launch_timed(kProfAttend, units, kern, dim3(1, (unsigned)a.n_seq), dim3(64 * kHeldWaves), held, st, one);
-    }
+        return launch_timed(kProfAttend, units, kern, dim3(1, (unsigned)a.n_seq), dim3(64 * W), lds, st, one);
+    };
+    const int whole_by = held_waves(D * (int)sizeof(T), D, sizeof(T) == 2 ? 32 : 16, p.waves, a);
+    if (whole_by == 8) return whole(std::integral_constant<int, 8>{});
+    if constexpr (sizeof(T) == 2) { if (whole_by == 4) return whole(std::integral_constant<int, 4>{}); }
     if (past) {
         if (p.waves == 8) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 8, true, false, kLogitsOut>, grid, dim3(512), 0, st, a);
         else if constexpr (sizeof(T) == 2) e = launch_timed(kProfAttend, units, attend_kernel<T, D, 1, 4, true, false, kLogitsOut>, grid, dim3(256), 0, st, a);

@@ -145,6 +145,7 @@ MASS = [  # dtype, d, n_seq, count, g, nq, visible, decay
     (BF16, 128, 3, 2000, 1, 500, 1501, 1.0), (BF16, 64, 1, 640, 8, 640, -3, 0.0),
     (BF16, 128, 161, 2001, 4, 1, None, 0.5), (BF16, 64, 330, 77, 4, 2, None, 1.0), (F32, 128, 170, 777, 16, 1, None, 0.0), (F32, 64, 165, 1001, 1, 1, None, 1.0),
     (BF16, 128, 160, 8768, 4, 1, None, 1.0), (BF16, 128, 160, 9100, 4, 1, None, 1.0), (BF16, 128, 600, 1, 3, 1, None, 1.0), (BF16, 128, 5, 513, 2, 1, None, 1.0),
+    (BF16, 128, 300, 400, 3, 1, None, 0.9), (BF16, 64, 520, 999, 4, 1, None, 1.0), (BF16, 64, 1500, 130, 1, 7, None, 0.0), (BF16, 128, 500, 4000, 4, 1, None, 1.0),
     (BF16, 128, 5, 512, 2, 8, None, 1.0), (F32, 128, 5, 256, 5, 3, None, 1.0), (F32, 128, 5, 257, 5, 3, None, 1.0), (BF16, 64, 5, 1024, 1, 7, None, 1.0),
 ]
 
@@ -393,6 +394,37 @@ def test_captured_and_on_another_stream(bk):
     graphs[0].replay()
     torch.cuda.synchronize()
     assert same(held[0], fresh)
+
+
+def test_whole_sequences_captured(bk):
+    """Logits of whole sequences in more LDS than a launch has by default, eviction in one launch, sequences of few own tokens: from a graph."""
+    p = bk.make_params(128, 64, 1, BF16, log_c=0.0)
+    gen, n, count = _gen(50), 256, 5000
+    K, V, w = _cache(gen, n, count, 128, BF16)
+    Q = torch.randn(n, 4, 1, 128, generator=gen, device="cuda").to(BF16)
+    ws = [torch.empty(k, device="cuda", dtype=torch.uint8) for k in (bk.attend_mass_workspace_bytes(p, n, count, 4, 1), bk.evict_workspace_bytes(p, n, count),
+                                                                     bk.attend_prefix_workspace_bytes(p, 8, 1024, 4, 1))]
+    own, Qo = _cache(gen, 1024, 9, 128, BF16), torch.randn(1024, 4, 1, 128, generator=gen, device="cuda").to(BF16)
+
+    def step(mass):
+        out, lse, got = bk.attend_mass(p, K, V, w, Q, mass, decay=0.5, workspace=ws[0])
+        kept = bk.evict(p, K, V, w, got, 300, n_sink=4, n_recent=64, workspace=ws[1])
+        pre = tuple(kept[k][:8] for k in ("K", "V", "w"))
+        z, l2 = bk.attend_prefix(p, pre, own, Qo, workspace=ws[2])
+        return out, lse, got, kept["idx"], kept["V"], z, l2
+
+    mass = torch.rand(n, count, generator=gen, device="cuda")
+    want = [t.clone() for t in step(mass)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step(mass)
+    for turn in range(3):
+        for t in held:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want)), turn
+        assert all(torch.equal(a, b) for a, b in zip(step(mass), want)), turn
 
 
 def test_caches_of_the_streaming_handle(bk):
