@@ -134,6 +134,25 @@ def test_prefix_sequences_without_tokens(bk, dtype, fan):
     assert bk.attend_prefix(p, pre, own, Q, lse=False)[1] is None
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("fan", [1, 5, 12, 40, 200])
+def test_an_infinite_value_shows_in_its_column(bk, dtype, fan):
+    """... of every query that meets it, whatever shares its workgroup, and in no other."""
+    gen, n_pre, cp, cs, d = _gen(fan), 2, 300, 40, 128
+    pre, own = _cache(gen, n_pre, cp, d, dtype, absent=0.0), _cache(gen, n_pre * fan, cs, d, dtype, absent=0.0)
+    for t in (pre[0], own[0]):
+        t.mul_(0.05)                                    # (logits near 0: no weight vanishes)
+    Q = (0.1 * torch.randn(n_pre * fan, 4, 1, d, generator=gen, device="cuda")).to(dtype)
+    p = bk.make_params(d, 64, 1, dtype, log_c=0.0)
+    ref, lse = bk.attend_prefix(p, pre, own, Q)
+    pre[1][0, 170, 5] = float("inf")
+    own[1][n_pre * fan - 1, 33, 77] = -float("inf")
+    out, lse2 = bk.attend_prefix(p, pre, own, Q)
+    assert torch.equal(lse, lse2) and bool((out[::2, :, :, 5] == float("inf")).all()) and bool((out[-1, :, :, 77] == -float("inf")).all())
+    out[::2, :, :, 5], out[-1, :, :, 77] = ref[::2, :, :, 5], ref[-1, :, :, 77]
+    assert torch.equal(out, ref)
+
+
 MASS = [  # dtype, d, n_seq, count, g, nq, visible, decay
     (BF16, 128, 1, 1, 1, 1, None, 1.0), (BF16, 128, 3, 31, 4, 1, None, 0.5), (BF16, 128, 2, 33, 8, 1, None, 0.0), (BF16, 64, 2, 129, 4, 2, None, 1.0),
     (BF16, 128, 2, 1000, 4, 1, None, 0.9), (BF16, 128, 1, 9000, 16, 1, None, 1.0), (BF16, 128, 2, 700, 2, 37, 664, 0.0), (BF16, 128, 1, 260, 4, 260, 1, 0.5),
