@@ -73,6 +73,7 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
         sees = visible(outer);
         most = visible((min(row_first + 32 * Q1, J.rows) - 1) / J.inner);
         t1 = min(t1, (most + KEYS - 1) / KEYS);
+        if (split > 0 && t0 >= t1) return;                           // (none of its queries sees this split: the merge does not look at it)
         sees_min = visible(min(row0, J.rows - 1) / J.inner);
     }
 
@@ -427,6 +428,12 @@ __device__ __forceinline__ void merge_rows(const TileArgs& a, const float* part,
     const int64_t row = block * ROWS + threadIdx.x / (LPR * SG);
     const bool there = row < a.n_rows;
     const int col = 4 * lane;
+    if (a.causal) {                                                  // the splits that this query sees something of (job 0 alone; head by head in memory)
+        const TileJob& J = a.job[0];
+        const int64_t sees = a.visible + (int)((uint32_t)row % (uint32_t)J.rows % (uint32_t)J.q_inner);
+        const int per = J.tiles_per_split * kTileKeys;
+        splits = (int)min((int64_t)splits, max((int64_t)1, (min(sees, (int64_t)J.count) + per - 1) / per));
+    }
     const float* src = part + (size_t)(there ? row : 0) * P;
     const size_t step = (size_t)a.n_rows * P;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
