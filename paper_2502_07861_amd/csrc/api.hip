@@ -484,7 +484,7 @@ int bkv_attend_prefix(const bkv_params* p, const void* K_p, const void* V_p, con
     if (count_s > 0) a.job[jobs++] = own;
     int64_t taken = 0;
     for (int k = jobs - 1; k >= 0; --k) {                  // (the own tokens first: the prefix is cut into what they leave room for)
-        bkv::tile_plan(a.job[k], row_bytes(p), elem_bytes(p), false, taken);
+        bkv::tile_plan(a.job[k], row_bytes(p), elem_bytes(p), false, taken, 0);
         taken += (int64_t)a.job[k].units * a.job[k].n_qt;
     }
     const hipError_t e = bkv::launch_tiles(p->dtype, p->d, a, jobs, (float*)workspace, st);
@@ -548,7 +548,7 @@ int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const
     char* ws = (char*)workspace;
     a.stats = (float*)ws;
     ws += align_up((size_t)n_seq * n_q * 8, 256);
-    bkv::tile_plan(j, row_bytes(p), elem_bytes(p), a.causal, 0);
+    bkv::tile_plan(j, row_bytes(p), elem_bytes(p), a.causal, 0, a.visible);
     hipError_t e = bkv::launch_tiles(p->dtype, p->d, a, 1, (float*)ws, st);
     if (e != hipSuccess) return hip_fail(e);
     const int splits = bkv::tile_most_splits(n_seq, n_q, elem_bytes(p), true);

@@ -260,7 +260,7 @@ struct TileArgs {
     uint32_t first;           // set by the launcher: workgroups of job 0
 };
 int tile_most_splits(int64_t n_streams, int64_t rows, int elem, bool causal);
-void tile_plan(TileJob& j, int row_bytes, int elem, bool causal, int64_t taken);
+void tile_plan(TileJob& j, int row_bytes, int elem, bool causal, int64_t taken, int64_t first);
 size_t tile_part_bytes(int d, int64_t n_rows, int splits);
 // part: room for the partial rows of all splits of all jobs, if they are more than one
 hipError_t launch_tiles(int dtype, int d, TileArgs& a, int n_jobs, float* part, hipStream_t st);

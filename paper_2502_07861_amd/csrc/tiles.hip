@@ -410,8 +410,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_kernel(const TileArgs a)
     const unsigned int turn = J.by_xcd ? in_xcd % (unsigned int)J.n_qt : block / units;
     if (unit >= units || turn >= (unsigned int)J.n_qt) return;
     const int qt = J.n_qt - 1 - (int)turn;                                      // (causal: the longest first)
-    const int split = (int)(unit % (unsigned int)J.splits);
-    const int64_t stream = unit / (unsigned int)J.splits;
+    const unsigned int splits = (unsigned int)J.splits;
+    // (causal: the first splits have the most to do, and where 2, 4 or 8 of them divide the XCDs among themselves, they take turns)
+    const int split = (int)((unit + (a.causal && 8u % splits == 0u ? unit >> 3 : 0u)) % splits);
+    const int64_t stream = unit / splits;
     if (J.qw == 4) tile_body<T, D, 4>(a, J, stream, split, qt, lds);
     else if (J.qw == 2) tile_body<T, D, 2>(a, J, stream, split, qt, lds);
     else if (J.qw == 1) tile_body<T, D, 1>(a, J, stream, split, qt, lds);
@@ -507,20 +509,46 @@ int tile_most_splits(int64_t n_streams, int64_t rows, int elem, bool causal) {
     return wgs > 0 ? (int)max((int64_t)1, tile_target(elem, causal) / wgs) : 1;
 }
 
+static bool tile_by_xcd(int64_t units) { return units % 8 == 0 || units >= 48; }
+
+// Splits of a job with workgroups of 128 queries, at most `most`: the least of (rounds of workgroups, by the fullest XCD) x (tiles of a split and
+// what a workgroup takes to begin and to end) + what the merge reads, in times of a tile; two workgroups of a compute unit side by side
+// take 1.5 times (fp32 1.8, causal bf16, of different lengths, 1.3) what one does.  `seen`: tiles that a query sees on average.  Against as many
+// splits as give two workgroups a compute unit, at least eight tiles each (bf16), us a call: 8 sequences x 420 tokens x 8 x 420 queries bf16 42 -> 33,
+// 106 prefixes x 199 x 200 bf16 36 -> 31, 13 x 1959 x 1959 fp32 390 -> 297, 9 x 730 x 4 x 730 fp32 158 -> 136, 8 x 8704 x 256 49.6 -> 47.4; a few
+// lose up to 6 % (94 prefixes x 1543 x 34 bf16 32.5 -> 34.6).
+static int best_splits(int64_t n_streams, int n_qt, int tiles, int most, bool b16, bool causal, int seen) {
+    const float side = !b16 ? 0.9f : causal ? 0.65f : 0.75f, ends = b16 ? 4.f : 1.f, merge = b16 ? 0.011f : 0.0025f;
+    float least = 0.f;
+    int best = 1;
+    for (int k = 1; k <= most; k += most / 64 + 1) {
+        const int per = (tiles + k - 1) / k, s = (tiles + per - 1) / per;
+        const int64_t units = n_streams * s;
+        const bool mixed = s % 8 != 0 && (8 % s != 0 || units >= 8 * s);          // every XCD has all splits, early ones and late ones
+        const float share = causal && mixed ? fminf(1.f, ((float)seen / (float)per + 0.5f) / (float)s) : 1.f;
+        const float in_xcd = (float)(tile_by_xcd(units) ? (units + 7) / 8 * n_qt : (units * n_qt + 7) / 8) * share;
+        const float rounds = ceilf(in_xcd * (8.f / kTileFull));
+        float cost = (rounds <= 1.f ? 1.f : side * rounds) * ((float)per + ends) + merge * (float)(units * n_qt);
+        if (causal && s > 1) cost += ends;                                         // (the merge's launch; a prefix has one anyway)
+        if (k == 1 || cost < least) { least = cost; best = s; }
+    }
+    return best;
+}
+
 // Queries of a workgroup and cuts of the keys.  Workgroups of 128 queries read the fewest keys; where they do not give every compute
-// unit one even with the keys cut, smaller ones are taken.  A cut of a workgroup of 128 queries costs 128 rows of sums written and
-// read, on bf16 about what two tiles of 64 keys take, so it gets eight of those where there are workgroups enough (in fp32 a tile takes
-// four times as long and no minimum is kept).  taken: workgroups of the launch that others have.
-void tile_plan(TileJob& j, int row_bytes, int elem, bool causal, int64_t taken) {
+// unit one even with the keys cut, smaller ones are taken.  taken: workgroups of the launch that others have; first: places that the first
+// query of a causal job sees.
+void tile_plan(TileJob& j, int row_bytes, int elem, bool causal, int64_t taken, int64_t first) {
     const int tiles = (j.count + kTileKeys - 1) / kTileKeys;
+    const int seen = (int)(((max(min(first, (int64_t)j.count), (int64_t)0) + j.count) / 2 + kTileKeys - 1) / kTileKeys);     // tiles, on average
     for (j.qw = tile_qw(j.rows);; j.qw /= 2) {
         const int64_t wgs = tile_units(j.n_streams, j.rows, j.qw);
         j.n_qt = (j.rows + 32 * j.qw - 1) / (32 * j.qw);
         // (A few others that the chip has no place for beside these cost a second round: 512 + 32 workgroups, two a compute unit, 11.6 us,
         // 256 + 32 of them with twice the keys 7.7.  Many others are the launch's work themselves.)
         int64_t splits = (tile_target(elem, causal) - (taken <= kTileTarget / 8 ? taken : 0)) / wgs;
-        if (j.qw == 4 && elem == 2) splits = min(splits, max((int64_t)(tiles + 7) / 8, (kTileFull + wgs - 1) / wgs));
         splits = max((int64_t)1, min(splits, (int64_t)tiles));
+        if (j.qw == 4 && tiles > 1) splits = best_splits(j.n_streams, j.n_qt, tiles, (int)splits, elem == 2, causal, seen);
         j.tiles_per_split = (int)((tiles + splits - 1) / splits);
         j.splits = j.tiles_per_split > 0 ? (tiles + j.tiles_per_split - 1) / j.tiles_per_split : 1;
         if (j.qw == 1 || wgs * j.splits >= kTileFull * 3 / 4) break;
@@ -535,7 +563,7 @@ void tile_plan(TileJob& j, int row_bytes, int elem, bool causal, int64_t taken) 
         j.qw = 0; j.n_qt = 1; j.splits = 1; j.tiles_per_split = 8;             // (tiles of 32 keys)
         j.units = (j.n_streams + per - 1) / per;
     }
-    j.by_xcd = j.units % 8 == 0 || j.units >= 48;
+    j.by_xcd = tile_by_xcd(j.units);
 }
 
 size_t tile_part_bytes(int d, int64_t n_rows, int splits) { return (size_t)n_rows * splits * (d + kTilePad) * sizeof(float); }

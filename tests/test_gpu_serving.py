@@ -164,6 +164,7 @@ MASS = [  # dtype, d, n_seq, count, g, nq, visible, decay
     (BF16, 128, 3, 2000, 1, 500, 1501, 1.0), (BF16, 64, 1, 640, 8, 640, -3, 0.0),
     (BF16, 128, 161, 2001, 4, 1, None, 0.5), (BF16, 64, 330, 77, 4, 2, None, 1.0), (F32, 128, 170, 777, 16, 1, None, 0.0), (F32, 64, 165, 1001, 1, 1, None, 1.0),
     (BF16, 128, 160, 8768, 4, 1, None, 1.0), (BF16, 128, 160, 9100, 4, 1, None, 1.0), (BF16, 128, 600, 1, 3, 1, None, 1.0), (BF16, 128, 5, 513, 2, 1, None, 1.0),
+    (BF16, 128, 2, 64, 4, 40, -1000, 1.0), (F32, 64, 3, 300, 9, 30, -31, 0.5), (BF16, 128, 8, 420, 8, 420, 1, 1.0), (BF16, 64, 2, 530, 4, 300, 100, 1.0),
     (BF16, 128, 300, 400, 3, 1, None, 0.9), (BF16, 64, 520, 999, 4, 1, None, 1.0), (BF16, 64, 1500, 130, 1, 7, None, 0.0), (BF16, 128, 500, 4000, 4, 1, None, 1.0),
     (BF16, 128, 5, 512, 2, 8, None, 1.0), (F32, 128, 5, 256, 5, 3, None, 1.0), (F32, 128, 5, 257, 5, 3, None, 1.0), (BF16, 64, 5, 1024, 1, 7, None, 1.0),
 ]
