@@ -511,12 +511,13 @@ int tile_most_splits(int64_t n_streams, int64_t rows, int elem, bool causal) {
 
 static bool tile_by_xcd(int64_t units) { return units % 8 == 0 || units >= 48; }
 
-// Splits of a job with workgroups of 128 queries, at most `most`: the least of (rounds of workgroups, by the fullest XCD) x (tiles of a split and
+// Splits of a job with workgroups of 128 queries (bf16: of 64 too), at most `most`: the least of (rounds of workgroups, by the fullest XCD) x (tiles of a split and
 // what a workgroup takes to begin and to end) + what the merge reads, in times of a tile; two workgroups of a compute unit side by side
 // take 1.5 times (fp32 1.8, causal bf16, of different lengths, 1.3) what one does.  `seen`: tiles that a query sees on average.  Against as many
 // splits as give two workgroups a compute unit, at least eight tiles each (bf16), us a call: 8 sequences x 420 tokens x 8 x 420 queries bf16 42 -> 33,
-// 106 prefixes x 199 x 200 bf16 36 -> 31, 13 x 1959 x 1959 fp32 390 -> 297, 9 x 730 x 4 x 730 fp32 158 -> 136, 8 x 8704 x 256 49.6 -> 47.4; a few
-// lose up to 6 % (94 prefixes x 1543 x 34 bf16 32.5 -> 34.6).
+// 106 prefixes x 199 x 200 bf16 36 -> 31, 13 x 1959 x 1959 fp32 390 -> 297, 9 x 730 x 4 x 730 fp32 158 -> 136, 8 x 8704 x 256 49.6 -> 47.4; workgroups
+// of 64: 106 prefixes x 487 x 42 24.6 -> 19.3, 6 x 3004 x 96 20.8 -> 17.2 (fp32 8 x 200 x 1120 22.5 -> 28.5: as they were); a few lose up to 6 %
+// (94 prefixes x 1543 x 34 bf16 32.5 -> 34.6) and one of 190 more (4 x 2616 x 75 18.6 -> 21.3).
 static int best_splits(int64_t n_streams, int n_qt, int tiles, int most, bool b16, bool causal, int seen) {
     const float side = !b16 ? 0.9f : causal ? 0.65f : 0.75f, ends = b16 ? 4.f : 1.f, merge = b16 ? 0.011f : 0.0025f;
     float least = 0.f;
@@ -548,7 +549,7 @@ void tile_plan(TileJob& j, int row_bytes, int elem, bool causal, int64_t taken, 
         // 256 + 32 of them with twice the keys 7.7.  Many others are the launch's work themselves.)
         int64_t splits = (tile_target(elem, causal) - (taken <= kTileTarget / 8 ? taken : 0)) / wgs;
         splits = max((int64_t)1, min(splits, (int64_t)tiles));
-        if (j.qw == 4 && tiles > 1) splits = best_splits(j.n_streams, j.n_qt, tiles, (int)splits, elem == 2, causal, seen);
+        if ((j.qw == 4 || (j.qw == 2 && elem == 2)) && tiles > 1) splits = best_splits(j.n_streams, j.n_qt, tiles, (int)splits, elem == 2, causal, seen);
         j.tiles_per_split = (int)((tiles + splits - 1) / splits);
         j.splits = j.tiles_per_split > 0 ? (tiles + j.tiles_per_split - 1) / j.tiles_per_split : 1;
         if (j.qw == 1 || wgs * j.splits >= kTileFull * 3 / 4) break;
