@@ -501,7 +501,7 @@ static int tile_qw(int64_t rows) { return rows > 64 ? 4 : rows > 32 ? 2 : 1; }
 static int64_t tile_units(int64_t n_streams, int64_t rows, int qw) { return n_streams * ((rows + 32 * qw - 1) / (32 * qw)); }
 
 // Splits of a job of this shape at most (any token count; with fewer queries to a workgroup there are more workgroups, and fewer splits).
-// Causal jobs in fp32 are cut twice as fine, as about half of their workgroups have little or nothing to do (1235 x 4 queries on 1235
+// Causal jobs in fp32 may be cut twice as fine, as about half of their workgroups have little or nothing to do (1235 x 4 queries on 1235
 // tokens, 3 sequences, d = 128: 97 -> 75 us; bf16, whose cuts cost more than their work, 3156 x 4 queries: 60 -> 68).
 static int64_t tile_target(int elem, bool causal) { return elem == 4 && causal ? 2 * kTileTarget : kTileTarget; }
 int tile_most_splits(int64_t n_streams, int64_t rows, int elem, bool causal) {
