@@ -216,8 +216,7 @@ int bkv_attend_kv_static(const bkv_params* p, const void* K_c, const void* V_c, 
  *               A count may be 0 (its pointers are then not looked at).  A place whose weight is not above 0 holds no token,
  *               whatever its rows hold (infinities and NaN too): sequences of different lengths share a count that way.
  * Q, out, lse_out  as in bkv_attend_kv; out must not overlap Q.  A query that meets no token gives zeros and lse = -inf.
- * Precision as in bkv_attend_kv, but with BKV_BF16 and more than 64 queries on a cache (a prefix's are those of all its
- * sequences) a weight may multiply its value row as one bf16 number (relative error <= 2^-8); lse_out is not affected.
+ * Precision as in bkv_attend_kv, however many sequences share a prefix.
  * The workspace may hold anything; calls that overlap in time must not share one.
  * Limits: n_seq <= 65535, g * nq <= 262140, n_seq * g * nq <= 2^31 - 256, counts <= 2^30 (else BKV_ESHAPE).                 */
 size_t bkv_attend_prefix_workspace_bytes(const bkv_params* p, int64_t n_pre, int64_t n_seq, int32_t g,

@@ -44,11 +44,6 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
     constexpr int SHARE = SOLO ? KEYS : KEYS / 4, STEPS = SHARE / F::kRps;        // rows of a tile that a wavefront brings
     // wavefronts a query has; groups of 32 keys a wavefront takes of a tile at a time, times (fp32: registers)
     constexpr int KW = SOLO ? 1 : 4 / Q1, NS = QW == 4 && R::kB16 ? 2 : 1, TIMES = QW == 4 ? 2 / NS : 1;
-    // bf16: a weight multiplies its value row as two bf16 numbers, its upper bits and what they leave (relative error 2^-17; the second
-    // one of a weight is never 0, so that an infinite value stays infinite), except
-    // for full workgroups of 128 queries, where the matrix cores are the bound: there it is rounded to one (2^-8), as the result is.
-    // 8 prefixes x 16385 tokens x 1280 queries: 165 -> 137 us, off the 64-bit result 1.7e-3 -> 2.1e-3 (rounding it makes 1.7e-3).
-    constexpr bool kTwo = R::kB16 && QW < 4;
 
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -237,7 +232,8 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
         for (int u = 0; u < NS; ++u)
 #pragma unroll
             for (int r = 0; r < 16; ++r) { s[u][r] = fast_exp2(fmaf(s[u][r], a.scale_log2, shift)); l += s[u][r]; }
-        // ---- values
+        // ---- values.  bf16: a weight multiplies its value row as two bf16 numbers, its upper bits and what they leave (relative error 2^-17,
+        // for any number of queries; the second one of a weight is never 0, so that an infinite value stays infinite)
 #pragma unroll
         for (int u = 0; u < NS; ++u) {
             if constexpr (R::kB16) {
@@ -247,16 +243,11 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float p0 = s[u][8 * j + 2 * i], p1 = s[u][8 * j + 2 * i + 1];
-                        if constexpr (kTwo) {
-                            const unsigned int b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
-                            x[i] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
-                            const floatx2 rest = {fmaf(p0, 0x1p-40f, p0 - __uint_as_float(b0 & 0xffff0000u)),
-                                                  fmaf(p1, 0x1p-40f, p1 - __uint_as_float(b1 & 0xffff0000u))};
-                            y[i] = __builtin_bit_cast(unsigned int, __builtin_convertvector(rest, bf16x2_tile));
-                        } else {
-                            const floatx2 both = {p0, p1};
-                            x[i] = __builtin_bit_cast(unsigned int, __builtin_convertvector(both, bf16x2_tile));
-                        }
+                        const unsigned int b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+                        x[i] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+                        const floatx2 rest = {fmaf(p0, 0x1p-40f, p0 - __uint_as_float(b0 & 0xffff0000u)),
+                                              fmaf(p1, 0x1p-40f, p1 - __uint_as_float(b1 & 0xffff0000u))};
+                        y[i] = __builtin_bit_cast(unsigned int, __builtin_convertvector(rest, bf16x2_tile));
                     }
 #pragma unroll
                     for (int e = 0; e < EPN; ++e) {
@@ -266,7 +257,7 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
                         struct { shortx4 a, b; } both = {v0, v1};
                         const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, both);
                         o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8_t, x), o[e], 0, 0, 0);
-                        if constexpr (kTwo) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8_t, y), o[e], 0, 0, 0);
+                        o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8_t, y), o[e], 0, 0, 0);
                     }
                 }
             } else {

@@ -1,0 +1,48 @@
+"""attend_prefix, attend_mass and evict where their arguments are unusual: against a plain implementation in 64 bits, with the bounds of
+test_gpu_serving.py."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_serving import BF16, F32, _attention, _cache, _check_mass, _check_out, _gen, bk  # noqa: F401  (bk: a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def _paired(gen, n_seq, n, d, dtype):
+    """Tokens in pairs: the same key, opposite values, weights 1 and 1 + delta, delta in 2^-9 .. 2^-7.  The answer is the small difference that
+    deltas leave, so the rounding of the weights shows in it and its own rounding does not."""
+    K = (0.2 * torch.randn(n_seq, n // 2, d, generator=gen, device="cuda")).to(dtype).repeat_interleave(2, dim=1)
+    V = torch.randn(n_seq, n // 2, d, generator=gen, device="cuda").to(dtype).repeat_interleave(2, dim=1)
+    V[:, 1::2] *= -1.0
+    w = torch.ones(n_seq, n, device="cuda")
+    w[:, 1::2] += torch.exp2(-9.0 + 2.0 * torch.rand(n_seq, n // 2, generator=gen, device="cuda"))
+    return K, V, w
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("n_pre,fan,g,nq", [(2, 1, 1, 1), (2, 3, 4, 1), (2, 8, 4, 2), (2, 33, 4, 5), (100, 15, 4, 1), (100, 33, 4, 1), (40, 33, 4, 5)])
+def test_an_answer_is_as_exact_in_any_company(bk, dtype, d, n_pre, fan, g, nq):  # noqa: F811
+    """The weights' 2^-16 holds whatever the number of queries that share a prefix."""
+    gen, cp, cs = _gen(fan + d), 200, 40
+    pre, own = _paired(gen, n_pre, cp, d, dtype), _paired(gen, n_pre * fan, cs, d, dtype)
+    Q = (0.2 * torch.randn(n_pre * fan, g, nq, d, generator=gen, device="cuda")).to(dtype)
+    out, lse = bk.attend_prefix(bk.make_params(d, 64, 1, dtype, log_c=0.0), pre, own, Q)
+    for s in range(0, n_pre * fan, max(1, n_pre * fan // 40)):
+        K, V, w = (torch.cat([a[s % n_pre], b[s]]) for a, b in zip(pre, own))
+        _check_out(out[s], lse[s], _attention(Q[s].reshape(-1, d), K, V, w), dtype, cp + cs, "sequence %d" % s)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("n_seq,g,nq,visible", [(2, 4, 1, None), (2, 4, 20, None), (3, 4, 64, 137), (200, 4, 32, None), (150, 4, 64, 137), (40, 4, 200, 1)])
+def test_an_answer_is_as_exact_whatever_is_asked_beside_it(bk, dtype, d, n_seq, g, nq, visible):  # noqa: F811
+    gen, count = _gen(nq + d), 200
+    K, V, w = _paired(gen, n_seq, count, d, dtype)
+    Q = (0.2 * torch.randn(n_seq, g, nq, d, generator=gen, device="cuda")).to(dtype)
+    out, lse, mass = bk.attend_mass(bk.make_params(d, 64, 1, dtype, log_c=0.0), K, V, w, Q, visible=visible)
+    sees = None if visible is None else (visible + torch.arange(nq, device="cuda")).repeat(g)
+    for s in range(0, n_seq, max(1, n_seq // 10)):
+        ref = _attention(Q[s].reshape(-1, d), K[s], V[s], w[s], sees)
+        _check_out(out[s], lse[s], ref, dtype, count, "sequence %d" % s)
+        _check_mass(mass[s], mass[s], 0.0, ref, count, g * nq, "sequence %d" % s)
