@@ -172,7 +172,8 @@ int bkv_merge_reduce_protected(const bkv_params* p, const void* K, const void* V
 
 /* ---- Alg. 1 output line on a flat weighted cache -------------------------------------------------
  * K_c, V_c      [n_seq, stride_tokens, d] device; only the first `count` tokens of each sequence
- *               are read.  w [n_seq, stride_tokens] fp32 (2^level; w == 0 marks an absent token).
+ *               are read.  w [n_seq, stride_tokens] fp32 (2^level; w == 0 marks an absent token, and
+ *               a subnormal weight counts as 0).
  * Q             [n_seq, g, nq, d]: g query heads share each KV sequence (GQA), nq queries each.
  * out           [n_seq, g, nq, d] (dtype as params);  lse_out [n_seq, g, nq] fp32 or NULL: natural
  *               log of the estimator's denominator, so partial results over disjoint token ranges
@@ -215,6 +216,7 @@ int bkv_attend_kv_static(const bkv_params* p, const void* K_c, const void* V_c, 
  * K_s, V_s      [n_seq, stride_s, d], w_s [n_seq, stride_s]: the first count_s places of every sequence are read.
  *               A count may be 0 (its pointers are then not looked at).  A place whose weight is not above 0 holds no token,
  *               whatever its rows hold (infinities and NaN too): sequences of different lengths share a count that way.
+ *               Subnormal weights are weights like all others.
  * Q, out, lse_out  as in bkv_attend_kv; out must not overlap Q.  A query that meets no token gives zeros and lse = -inf.
  * Precision as in bkv_attend_kv, however many sequences share a prefix.
  * The workspace may hold anything; calls that overlap in time must not share one.

@@ -138,6 +138,11 @@ __device__ __forceinline__ unsigned int f32_to_bf16_bits(float x) {
 }
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+// log2 of a token weight: v_log_f32 takes a subnormal number for 0, 2^32 times as much it is none
+__device__ __forceinline__ float log2_weight(float w) {
+    const bool small = w < 0x1p-126f;
+    return __builtin_amdgcn_logf(small ? w * 0x1p32f : w) - (small ? 32.f : 0.f);
+}
 
 // Cross-lane steps without LDS: DPP inside a row of 16 lanes, v_permlane16_swap / v_permlane32_swap between rows
 // (__shfl_xor goes through LDS: about 130 clocks a step, and a reduction is a chain of six).

@@ -99,7 +99,7 @@ __global__ __launch_bounds__(kMassThreads, sizeof(T) == 2 ? 3 : 1) void mass_ker
             for (int c = 0; c < R::kPieces; ++c)
                 if (!live) kf[c] = uintx4{0u, 0u, 0u, 0u};           // (whatever the row holds)
         }
-        const float mine = live ? __builtin_amdgcn_logf(w) * a.inv_scale : kTileDead;
+        const float mine = live ? log2_weight(w) * a.inv_scale : kTileDead;
 #pragma unroll
         for (int r = 0; r < 16; ++r) bias[r] = __shfl(mine, tile_row(r, h));
     }

@@ -190,9 +190,9 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
         // parts (together all its bits) times ones, in the half of the wavefront that holds the group's keys
         const float first = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(w)));
         const bool one = first > 0.f && __ballot(w == first) == ~0ull;
-        const float b = one ? __builtin_amdgcn_logf(first) : 0.f;
+        const float b = one ? log2_weight(first) : 0.f;
         if (!one) {
-            const float x = w > 0.f ? __builtin_amdgcn_logf(w) * a.inv_scale : kTileDead;
+            const float x = w > 0.f ? log2_weight(w) * a.inv_scale : kTileDead;
 #pragma unroll
             for (int u = 0; u < NS; ++u) {
                 const float y = h == ksub + group + u ? x : 0.f;

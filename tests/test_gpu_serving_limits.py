@@ -46,3 +46,50 @@ def test_an_answer_is_as_exact_whatever_is_asked_beside_it(bk, dtype, d, n_seq, 
         ref = _attention(Q[s].reshape(-1, d), K[s], V[s], w[s], sees)
         _check_out(out[s], lse[s], ref, dtype, count, "sequence %d" % s)
         _check_mass(mass[s], mass[s], 0.0, ref, count, g * nq, "sequence %d" % s)
+
+
+# Token weights: subnormal ones are tokens like all others.  "far": beside weights up to 2^60; "small": subnormal ones alone; "equal": all the same
+# subnormal number; "few": one subnormal token in a tile of ordinary ones.
+def _odd_weights(gen, shape, kind):
+    rand = lambda: torch.rand(*shape, generator=gen, device="cuda")
+    if kind == "equal":
+        return torch.full(shape, 2.0 ** -130, device="cuda")
+    small = (1.0 + torch.floor(rand() * 1e6)) * 2.0 ** -149
+    if kind == "small":
+        return small
+    if kind == "few":
+        return torch.where(rand() < 0.02, small, torch.ones(shape, device="cuda"))
+    far = torch.exp2(torch.floor(rand() * 121.0) - 60.0)
+    return torch.where(rand() < 0.3, small, far)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("kind", ["far", "small", "equal", "few"])
+@pytest.mark.parametrize("n_seq,count,g,nq,visible", [(2, 300, 4, 1, None), (2, 3000, 4, 1, None), (200, 100, 4, 1, None), (2, 300, 4, 9, None),
+                                                      (1, 300, 4, 40, None), (2, 130, 1, 130, 1), (300, 40, 4, 7, None)])
+def test_mass_of_subnormal_weights(bk, dtype, d, kind, n_seq, count, g, nq, visible):  # noqa: F811
+    gen = _gen(count + nq)
+    K, V, w = _cache(gen, n_seq, count, d, dtype, absent=0.0)
+    w = _odd_weights(gen, (n_seq, count), kind)
+    Q = torch.randn(n_seq, g, nq, d, generator=gen, device="cuda").to(dtype)
+    out, lse, mass = bk.attend_mass(bk.make_params(d, 64, 1, dtype, log_c=0.0), K, V, w, Q, visible=visible)
+    sees = None if visible is None else (visible + torch.arange(nq, device="cuda")).repeat(g)
+    for s in range(0, n_seq, max(1, n_seq // 5)):
+        ref = _attention(Q[s].reshape(-1, d), K[s], V[s], w[s], sees)
+        _check_out(out[s], lse[s], ref, dtype, count, "sequence %d" % s)
+        _check_mass(mass[s], mass[s], 0.0, ref, count, g * nq, "sequence %d" % s)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("kind", ["far", "small", "equal", "few"])
+@pytest.mark.parametrize("n_pre,fan,g", [(2, 3, 4), (1, 9, 4), (1, 40, 4), (150, 2, 1)])
+def test_prefix_of_subnormal_weights(bk, dtype, d, kind, n_pre, fan, g):  # noqa: F811
+    gen, n_seq, cp, cs = _gen(fan), n_pre * fan, 150, 50
+    pre, own = list(_cache(gen, n_pre, cp, d, dtype, absent=0.0)), list(_cache(gen, n_seq, cs, d, dtype, absent=0.0))
+    pre[2], own[2] = _odd_weights(gen, (n_pre, cp), kind), _odd_weights(gen, (n_seq, cs), kind)
+    Q = torch.randn(n_seq, g, 1, d, generator=gen, device="cuda").to(dtype)
+    p = bk.make_params(d, 64, 1, dtype, log_c=0.0)
+    out, lse = bk.attend_prefix(p, pre, own, Q)
+    for s in range(0, n_seq, max(1, n_seq // 10)):
+        K, V, w = (torch.cat([a[s % n_pre], b[s]]) for a, b in zip(pre, own))
+        _check_out(out[s], lse[s], _attention(Q[s].reshape(-1, d), K, V, w), dtype, cp + cs, "sequence %d" % s)
