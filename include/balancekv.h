@@ -216,7 +216,7 @@ int bkv_attend_kv_static(const bkv_params* p, const void* K_c, const void* V_c, 
  * K_s, V_s      [n_seq, stride_s, d], w_s [n_seq, stride_s]: the first count_s places of every sequence are read.
  *               A count may be 0 (its pointers are then not looked at).  A place whose weight is not above 0 holds no token,
  *               whatever its rows hold (infinities and NaN too): sequences of different lengths share a count that way.
- *               Subnormal weights are weights like all others.
+ *               Subnormal weights are weights like all others; one of +inf gives NaN to the queries that meet it.
  * Q, out, lse_out  as in bkv_attend_kv; out must not overlap Q.  A query that meets no token gives zeros and lse = -inf.
  * Precision as in bkv_attend_kv, however many sequences share a prefix.
  * The workspace may hold anything; calls that overlap in time must not share one.

@@ -187,9 +187,10 @@ __device__ __forceinline__ void tile_body(const TileArgs& a, const TileJob& J, i
         }
         __builtin_amdgcn_s_setprio(0);
         // ---- token weights: one for the whole tile (the usual tile), or ln2 w of every key as one more product: its three bf16
-        // parts (together all its bits) times ones, in the half of the wavefront that holds the group's keys
+        // parts (together all its bits) times ones, in the half of the wavefront that holds the group's keys.  An infinite weight makes NaN of
+        // the queries that see its token, so it is never the tile's
         const float first = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(w)));
-        const bool one = first > 0.f && __ballot(w == first) == ~0ull;
+        const bool one = first > 0.f && first < INFINITY && __ballot(w == first) == ~0ull;
         const float b = one ? log2_weight(first) : 0.f;
         if (!one) {
             const float x = w > 0.f ? log2_weight(w) * a.inv_scale : kTileDead;

@@ -93,3 +93,20 @@ def test_prefix_of_subnormal_weights(bk, dtype, d, kind, n_pre, fan, g):  # noqa
     for s in range(0, n_seq, max(1, n_seq // 10)):
         K, V, w = (torch.cat([a[s % n_pre], b[s]]) for a, b in zip(pre, own))
         _check_out(out[s], lse[s], _attention(Q[s].reshape(-1, d), K, V, w), dtype, cp + cs, "sequence %d" % s)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n_seq,nq,first", [(2, 30, 55), (2, 190, -25), (2, 100, 40), (200, 100, 40), (200, 130, 20)])
+def test_an_infinite_weight_reaches_those_that_see_it(bk, dtype, n_seq, nq, first):  # noqa: F811
+    """inf / inf for every query that sees the token, nothing for the others, also where a whole tile weighs that much."""
+    gen, d = _gen(nq), 128
+    K, V, w = _cache(gen, n_seq, 200, d, dtype, absent=0.1, poison=False)
+    Q = torch.randn(n_seq, 1, nq, d, generator=gen, device="cuda").to(dtype)
+    p = bk.make_params(d, 64, 1, dtype, log_c=0.0)
+    ref, lse, _ = bk.attend_mass(p, K, V, w, Q, visible=first)
+    w[:, 64:128] = float("inf")
+    out, lse2, _ = bk.attend_mass(p, K, V, w, Q, visible=first)
+    before = 64 - first + 1                                      # queries that see 64 places at most
+    assert 0 < before < nq
+    assert torch.equal(out[:, :, :before], ref[:, :, :before]) and torch.equal(lse[:, :, :before], lse2[:, :, :before])
+    assert bool(out[:, :, before:].isnan().all()) and bool(lse2[:, :, before:].isnan().all())
