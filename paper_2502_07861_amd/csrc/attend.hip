@@ -83,7 +83,8 @@ template <typename T> __device__ __forceinline__ void store4(char* out, size_t i
 // ns0 .. ns0 + ns1 - 1 belong to the second set.  Whole workgroup of NTH threads; a thread owns four columns of a query and
 // every SR-th split, with a running reference of its own, so that one pass of independent loads is all the latency there is;
 // the order of all sums is fixed.
-template <typename T, int D, int NTH>
+// NANS: the lse of a query with a NaN is NaN (attend_kv gives -inf).
+template <typename T, int D, int NTH, bool NANS = false>
 __device__ __forceinline__ void merge_rows(const float* part, size_t sstride, int nq, int ns0, int ns1, char* out, float* lse_out,
                                            size_t row0, float* red /*[NTH * 8]*/) {
     constexpr int P = D + kRowPad, CG = D / 4;
@@ -169,7 +170,7 @@ __device__ __forceinline__ void merge_rows(const float* part, size_t sstride, in
                 M = Md; L = Ld;
             }
             store4<T>(out, (row0 + q) * D + col, acc * f);
-            if (lse_out && col == 0) lse_out[row0 + q] = L > 0.f ? log2_or(L, M) * 0.6931471805599453f : -INFINITY;
+            if (lse_out && col == 0) lse_out[row0 + q] = (NANS ? L != 0.f : L > 0.f) ? log2_or(L, M) * 0.6931471805599453f : -INFINITY;
         }
     }
 }
@@ -689,12 +690,14 @@ __global__ __launch_bounds__(W * 64) void attend_kernel(const AttendArgs a) {
             if (has_v) acc += *reinterpret_cast<const floatx4*>(row + w * meet + col) * f;
         }
         if (ns == 1) {                          // the whole range was one split: normalise and store
-            store4<T>(a.out, (row0 + q) * D + col, acc * (L > 0.f ? 1.f / L : 0.f));
-            if (col == 0 && a.lse_out) a.lse_out[row0 + q] = L > 0.f ? log2_or(L, M) * 0.6931471805599453f : -INFINITY;
+            const bool some = LOGITS != 0 ? L != 0.f : L > 0.f;                // (LOGITS: NaN stays NaN, see merge_rows)
+            const float f = some ? 1.f / L : 0.f;
+            store4<T>(a.out, (row0 + q) * D + col, acc * f);
+            if (col == 0 && a.lse_out) a.lse_out[row0 + q] = some ? log2_or(L, M) * 0.6931471805599453f : -INFINITY;
             if constexpr (HELD) {
-                if (col == 0) *reinterpret_cast<floatx2*>(held_stats + 2 * q) = floatx2{M, L > 0.f ? 1.f / L : 0.f};
+                if (col == 0) *reinterpret_cast<floatx2*>(held_stats + 2 * q) = floatx2{M, f};
             } else if constexpr (LOGITS == kLogitsOut) {
-                if (col == 0) *reinterpret_cast<floatx2*>(a.stats + 2 * (row0 + q)) = floatx2{M, L > 0.f ? 1.f / L : 0.f};
+                if (col == 0) *reinterpret_cast<floatx2*>(a.stats + 2 * (row0 + q)) = floatx2{M, f};
             }
         } else {
             float* dst = part + split * sstride + q * P;
@@ -746,7 +749,7 @@ __global__ __launch_bounds__(kMergeThreads) void attend_mass_kernel(const Attend
     if (block < merge_blocks) {
         const int64_t seq = block / (uint32_t)a.n_q;
         const int q = (int)(block % (uint32_t)a.n_q);
-        merge_rows<T, D, kMergeThreads>(a.partial + (size_t)seq * ns * sstride + (size_t)q * P, sstride, 1, ns, 0, a.out, a.lse_out, (size_t)seq * a.n_q + q, red);
+        merge_rows<T, D, kMergeThreads, true>(a.partial + (size_t)seq * ns * sstride + (size_t)q * P, sstride, 1, ns, 0, a.out, a.lse_out, (size_t)seq * a.n_q + q, red);
         return;
     }
     block -= merge_blocks;
@@ -769,7 +772,7 @@ __global__ __launch_bounds__(kMergeThreads) void attend_mass_kernel(const Attend
             }
             const float all = wave_max(m);
             l = wave_sum(l * fast_exp2(m - all));
-            ml = floatx2{all, l > 0.f ? 1.f / l : 0.f};
+            ml = floatx2{all, l != 0.f ? 1.f / l : 0.f};
         } else ml = *reinterpret_cast<const floatx2*>(a.stats + 2 * ((size_t)seq * a.n_q + q));
         if (lane == 0) st[q] = ml;
     }

@@ -166,7 +166,8 @@ __global__ __launch_bounds__(kMassThreads, sizeof(T) == 2 ? 3 : 1) void mass_ker
         while (!step(std::integral_constant<int, 0>{}) && !step(std::integral_constant<int, 1>{})) {}
     }
     const int s = lane & 15;
-    const float total = xor_sum<16>(row16_transpose_sum(acc, s));
+    const bool live = __shfl(w, tile_row(s, h)) > 0.f;               // (a NaN query reaches no place without a token)
+    const float sum = xor_sum<16>(row16_transpose_sum(acc, s)), total = live ? sum : 0.f;
     const int to = k0 + tile_row(s, h);
     if ((lane & 16) != 0 || to >= a.count) return;
     if (a.splits > 1) {

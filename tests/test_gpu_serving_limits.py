@@ -110,3 +110,26 @@ def test_an_infinite_weight_reaches_those_that_see_it(bk, dtype, n_seq, nq, firs
     assert 0 < before < nq
     assert torch.equal(out[:, :, :before], ref[:, :, :before]) and torch.equal(lse[:, :, :before], lse2[:, :, :before])
     assert bool(out[:, :, before:].isnan().all()) and bool(lse2[:, :, before:].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n_seq,count,g,nq", [(2, 200, 4, 1), (2, 3000, 4, 1), (200, 2000, 4, 1), (2, 200, 4, 30), (2, 3000, 4, 30), (300, 50, 1, 17)])
+def test_a_query_of_nan(bk, dtype, n_seq, count, g, nq):  # noqa: F811
+    """Its answer, its lse and the masses of its sequence's tokens are NaN; places without a token, other queries and sequences stay as they are."""
+    gen, d = _gen(count), 128
+    K, V, w = _cache(gen, n_seq, count, d, dtype)
+    Q = torch.randn(n_seq, g, nq, d, generator=gen, device="cuda").to(dtype)
+    p = bk.make_params(d, 64, 1, dtype, log_c=0.0)
+    ref = bk.attend_mass(p, K, V, w, Q)
+    z, l = bk.attend_prefix(p, (K[:1], V[:1], w[:1]), (K, V, w), Q)
+    Q[1, g - 1, nq - 1, 5] = float("nan")
+    got = bk.attend_mass(p, K, V, w, Q)
+    z2, l2 = bk.attend_prefix(p, (K[:1], V[:1], w[:1]), (K, V, w), Q)
+    for (o, x), (o2, x2) in (((ref[0], ref[1]), (got[0], got[1])), ((z, l), (z2, l2))):
+        assert bool(o2[1, g - 1, nq - 1].isnan().all()) and bool(x2[1, g - 1, nq - 1].isnan())
+        o2[1, g - 1, nq - 1], x2[1, g - 1, nq - 1] = o[1, g - 1, nq - 1], x[1, g - 1, nq - 1]
+        assert torch.equal(o, o2) and torch.equal(x, x2)
+    live = w[1] > 0
+    assert bool(got[2][1][live].isnan().all()) and bool((got[2][1][~live] == 0).all())
+    got[2][1] = ref[2][1]
+    assert torch.equal(got[2], ref[2])
