@@ -217,8 +217,9 @@ int bkv_attend_kv_static(const bkv_params* p, const void* K_c, const void* V_c, 
  *               A count may be 0 (its pointers are then not looked at).  A place whose weight is not above 0 holds no token,
  *               whatever its rows hold (infinities and NaN too): sequences of different lengths share a count that way.
  *               Subnormal weights are weights like all others; one of +inf gives NaN to the queries that meet it.
- * Q, out, lse_out  as in bkv_attend_kv; out must not overlap Q.  A query that meets no token gives zeros and lse = -inf, one that
- *               holds a NaN gives NaN in out and lse.
+ * Q, out, lse_out  as in bkv_attend_kv.  A query that meets no token gives zeros and lse = -inf, one that holds a NaN gives NaN in
+ *               out and lse.
+ * BKV_EINVAL    too if out or lse_out lies on anything that is read, or on each other (between two sequences' places they may lie).
  * Precision as in bkv_attend_kv, however many sequences share a prefix.
  * The workspace may hold anything; calls that overlap in time must not share one.
  * Limits: n_seq <= 65535, g * nq <= 262140, n_seq * g * nq <= 2^31 - 256, counts <= 2^30 (else BKV_ESHAPE).                 */
@@ -240,8 +241,9 @@ int bkv_attend_prefix(const bkv_params* p, const void* K_p, const void* V_p, con
  *               itself: 1.  What places hold that no query sees does not matter; value rows of tokens that some queries see
  *               must be finite, as those that do not see them add them with weight 0.
  *               A query that holds a NaN makes the masses of its sequence's tokens NaN (those it does not see may be, too).
- * mass_in       [n_seq, stride_tokens] fp32 or NULL (zeros); may be mass_out, no other overlap.  decay in [0, 1]; with 0 it is
- *               not read.  mass_out [n_seq, stride_tokens]: places from `count` on are left as they are.  count == 0: untouched.
+ * mass_in       [n_seq, stride_tokens] fp32 or NULL (zeros); may be mass_out.  decay in [0, 1]; with 0 it is not read.
+ * mass_out      [n_seq, stride_tokens]: places from `count` on are left as they are.  count == 0: untouched.
+ * BKV_EINVAL    too for any other overlap of out, lse_out or mass_out with an input or with each other.
  * The sums run in an order that depends on the shapes alone: the same call gives the same bits.                             */
 size_t bkv_attend_mass_workspace_bytes(const bkv_params* p, int64_t n_seq, int64_t count, int32_t g, int32_t nq);
 int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const float* w, int64_t n_seq,

@@ -410,9 +410,41 @@ int bkv_attend_kv_static(const bkv_params* p, const void* K_c, const void* V_c, 
 // ------------------------------------------------------------------------------------------ serving: prefix, mass, eviction
 }  // extern "C"
 
-static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return a && b && na && nb && x < y + nb && y < x + na;
+// n stretches of len bytes, step bytes apart, from `at` on (null: nothing).
+struct Span { const void* at; size_t n, len, step; };
+static Span dense(const void* at, size_t bytes) { return {at, 1, bytes, bytes}; }
+// The first `count` of `stride` elements of every sequence.
+static Span cache_span(const void* at, int64_t n_seq, int64_t count, int64_t stride, size_t elem) {
+    return {at, (size_t)n_seq, (size_t)count * elem, (size_t)stride * elem};
+}
+
+// Does one of s's stretches reach into [lo, hi)?
+static bool reaches(const Span& s, uintptr_t lo, uintptr_t hi) {
+    const uintptr_t from = (uintptr_t)s.at;
+    if (lo >= hi || hi <= from) return false;
+    const size_t i = lo < from + s.len ? 0 : (lo - from - s.len) / s.step + 1;       // the first one that ends behind lo
+    return i < s.n && from + i * s.step < hi;
+}
+// (what lies between the stretches of one may hold the other; that far only if their hulls meet)
+static bool overlap(const Span& a, const Span& b) {
+    if (!a.at || !b.at || !a.n || !b.n || !a.len || !b.len) return false;
+    const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+    if (x >= y + (b.n - 1) * b.step + b.len || y >= x + (a.n - 1) * a.step + a.len) return false;
+    const Span &few = a.n < b.n ? a : b, &many = a.n < b.n ? b : a;
+    for (size_t i = 0; i < few.n; ++i) {
+        const uintptr_t lo = (uintptr_t)few.at + i * few.step;
+        if (reaches(many, lo, lo + few.len)) return true;
+    }
+    return false;
+}
+// Does one of the outputs lie on an input or on another output?
+template <size_t IN, size_t OUT>
+static bool outputs_overlap(const Span (&in)[IN], const Span (&out)[OUT]) {
+    for (size_t i = 0; i < OUT; ++i) {
+        for (size_t k = 0; k < IN; ++k) if (overlap(out[i], in[k])) return true;
+        for (size_t k = 0; k < i; ++k) if (overlap(out[i], out[k])) return true;
+    }
+    return false;
 }
 
 // The two jobs of a batch on shared prefixes; the fan-out is n_seq / n_pre.
@@ -466,8 +498,12 @@ int bkv_attend_prefix(const bkv_params* p, const void* K_p, const void* V_p, con
     if (count_p > (1 << 30) || count_s > (1 << 30)) return BKV_ESHAPE;
     if (!Q || !out || !aligned16(Q) || !aligned16(out)) return BKV_EINVAL;
     const int n_q = g * nq;
-    const size_t q_bytes = (size_t)n_seq * n_q * row_bytes(p);
-    if (overlap(Q, q_bytes, out, q_bytes)) return BKV_EINVAL;
+    const size_t rb = row_bytes(p), n_rows = (size_t)n_seq * n_q;
+    const Span in[] = {dense(Q, n_rows * rb),
+                       cache_span(K_p, n_pre, count_p, stride_p, rb), cache_span(V_p, n_pre, count_p, stride_p, rb), cache_span(w_p, n_pre, count_p, stride_p, 4),
+                       cache_span(K_s, n_seq, count_s, stride_s, rb), cache_span(V_s, n_seq, count_s, stride_s, rb), cache_span(w_s, n_seq, count_s, stride_s, 4)};
+    const Span res[] = {dense(out, n_rows * rb), dense(lse_out, n_rows * 4)};
+    if (outputs_overlap(in, res)) return BKV_EINVAL;
     hipStream_t st = (hipStream_t)hip_stream;
     if (count_p == 0 && count_s == 0) return fill_empty(p, n_seq * n_q, out, lse_out, st);
     if (count_p > 0 && (!K_p || !V_p || !w_p || !aligned16(K_p) || !aligned16(V_p))) return BKV_EINVAL;
@@ -512,14 +548,16 @@ int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const
     if (count > (1 << 30)) return BKV_ESHAPE;
     if (!Q || !out || !aligned16(Q) || !aligned16(out)) return BKV_EINVAL;
     const int n_q = g * nq;
-    const size_t q_bytes = (size_t)n_seq * n_q * row_bytes(p);
-    if (overlap(Q, q_bytes, out, q_bytes)) return BKV_EINVAL;
+    const size_t rb = row_bytes(p), n_rows = (size_t)n_seq * n_q;
     hipStream_t st = (hipStream_t)hip_stream;
+    if (count > 0 && (!K_c || !V_c || !w || !mass_out || !aligned16(K_c) || !aligned16(V_c))) return BKV_EINVAL;
+    const Span masses = cache_span(mass_out, n_seq, count, stride_tokens, 4);
+    const Span in[] = {dense(Q, n_rows * rb), cache_span(K_c, n_seq, count, stride_tokens, rb), cache_span(V_c, n_seq, count, stride_tokens, rb),
+                       cache_span(w, n_seq, count, stride_tokens, 4),
+                       cache_span(mass_in == mass_out ? nullptr : mass_in, n_seq, count, stride_tokens, 4)};        // (in place: `masses` stands for both)
+    const Span res[] = {dense(out, n_rows * rb), dense(lse_out, n_rows * 4), masses};
+    if (outputs_overlap(in, res)) return BKV_EINVAL;
     if (count == 0) return fill_empty(p, n_seq * n_q, out, lse_out, st);
-    if (!K_c || !V_c || !w || !mass_out || !aligned16(K_c) || !aligned16(V_c)) return BKV_EINVAL;
-    const size_t m_bytes = ((size_t)(n_seq - 1) * stride_tokens + count) * 4;
-    if (mass_in != mass_out && overlap(mass_in, m_bytes, mass_out, m_bytes)) return BKV_EINVAL;
-    if (overlap(w, m_bytes, mass_out, m_bytes)) return BKV_EINVAL;
     if (!workspace || ws_bytes < bkv_attend_mass_workspace_bytes(p, n_seq, count, g, nq) || !aligned16(workspace)) return BKV_EWORKSPACE;
     if (decay == 0.f) mass_in = nullptr;
     if (visible >= count && bkv::attend_keeps_logits(row_bytes(p), n_q)) {
@@ -586,13 +624,12 @@ int bkv_evict(const bkv_params* p, const void* K_c, const void* V_c, const float
     if (!K_c || !V_c || !w || !mass || !K_out || !V_out) return BKV_EINVAL;
     if (!aligned16(K_c) || !aligned16(V_c) || !aligned16(K_out) || !aligned16(V_out)) return BKV_EINVAL;
     // rows move in any order: no output may lie on anything that is read or written beside it
-    const size_t in_tok = (size_t)(n_seq - 1) * stride_tokens + count, out_tok = (size_t)n_seq * keep, rb = row_bytes(p);
-    const struct { const void* at; size_t n; } in[5] = {{K_c, in_tok * rb}, {V_c, in_tok * rb}, {w, in_tok * 4}, {mass, in_tok * 4}, {idx_in, in_tok * 4}},
-        res[6] = {{K_out, out_tok * rb}, {V_out, out_tok * rb}, {w_out, out_tok * 4}, {mass_out, out_tok * 4}, {idx_out, out_tok * 4}, {count_out, (size_t)n_seq * 4}};
-    for (int i = 0; i < 6; ++i) {
-        for (int k = 0; k < 5; ++k) if (overlap(res[i].at, res[i].n, in[k].at, in[k].n)) return BKV_EINVAL;
-        for (int k = 0; k < i; ++k) if (overlap(res[i].at, res[i].n, res[k].at, res[k].n)) return BKV_EINVAL;
-    }
+    const size_t out_tok = (size_t)n_seq * keep, rb = row_bytes(p);
+    const Span in[] = {cache_span(K_c, n_seq, count, stride_tokens, rb), cache_span(V_c, n_seq, count, stride_tokens, rb), cache_span(w, n_seq, count, stride_tokens, 4),
+                       cache_span(mass, n_seq, count, stride_tokens, 4), cache_span(idx_in, n_seq, count, stride_tokens, 4)};
+    const Span res[] = {dense(K_out, out_tok * rb), dense(V_out, out_tok * rb), dense(w_out, out_tok * 4), dense(mass_out, out_tok * 4),
+                        dense(idx_out, out_tok * 4), dense(count_out, (size_t)n_seq * 4)};
+    if (outputs_overlap(in, res)) return BKV_EINVAL;
     if (!workspace || ws_bytes < bkv_evict_workspace_bytes(p, n_seq, count) || !aligned16(workspace)) return BKV_EWORKSPACE;
     bkv::EvictArgs a;
     memset(&a, 0, sizeof(a));
