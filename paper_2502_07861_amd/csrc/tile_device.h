@@ -63,9 +63,14 @@ __device__ __forceinline__ float half_sum(float x) { return xor_sum<32>(x); }
 __device__ __forceinline__ unsigned int lds_address(const void* p) {
     return (unsigned int)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
 }
+// m0 is written: declared, so that nothing behind takes it for what it was (the compiler sets it for each use of its own, and warns that
+// it does not keep it across the statement, which nothing asks for).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void to_lds(const char* base, unsigned int off, unsigned int to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ void tile_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 // The same in the compiler's books too (which hold the loads it made itself): nothing behind it waits for those again.
 __device__ __forceinline__ void all_arrived_so_far() {
