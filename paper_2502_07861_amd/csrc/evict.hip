@@ -94,7 +94,13 @@ __device__ __forceinline__ int lanes_below(unsigned long long m) {
 
 // The places that stay, each to its own place of the list; `before` of them lie in front of this wavefront.
 template <int KPT>
-__device__ __forceinline__ void list_ranks(const unsigned int (&x)[KPT], const EvictCut& cut, int first, int32_t* pick, int2 before) {
+__device__ __forceinline__ void list_ranks(const unsigned int (&x)[KPT], EvictCut cut, int first, int32_t* pick, int2 before) {
+    // The compiler is not to know that it had these comparisons (sum_ranks) and places (load_ranks) before: kept, they take two scalar
+    // registers and most of a vector register a rank, and 64 ranks a thread went to memory for it.
+    first += place_of(KPT, 0);
+    cut.from = __builtin_amdgcn_readfirstlane(cut.from);
+    cut.equal = __builtin_amdgcn_readfirstlane(cut.equal);
+    asm("" : "+s"(cut.from), "+s"(cut.equal), "+v"(first));
 #pragma unroll
     for (int j = 0; j < KPT / 4; ++j) {
         int up = before.x, eq = before.y;
@@ -115,7 +121,7 @@ __device__ __forceinline__ void list_ranks(const unsigned int (&x)[KPT], const E
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const bool is_up = x[4 * j + e] >= cut.from, is_eq = cut.equal != 0u && x[4 * j + e] == cut.equal;
-            if (is_up || (is_eq && eq < cut.need)) pick[up + min(eq, cut.need)] = first + place_of(KPT, j) + e;
+            if (is_up || (is_eq && eq < cut.need)) pick[up + min(eq, cut.need)] = first + 256 * j + e;
             up += is_up; eq += is_eq;
         }
     }
@@ -359,7 +365,10 @@ __global__ __launch_bounds__(kSelectThreads) void evict_list_kernel(const EvictA
     if (blockIdx.x + 1 == gridDim.x) end_list(a, seq, total, cut);
 }
 
-constexpr int kOnePlaces = 64 * kSelectThreads;            // places whose ranks fit the registers of one workgroup
+// Places whose ranks fit the registers of one workgroup, 64 a thread; more of them take the search by many.  By one / by many, a quarter of the rows
+// kept, d = 128, bf16, us a call: 8 x 33000 41.5 / 46.7, 8 x 65536 54 / 59, 64 x 65536 217 / 240, 256 x 33000 405 / 484, 256 x 65536 793 / 929; by many alone:
+// 8 x 131072 82 (3.4 TB/s read and written), 512 x 131072 3900 (4.6).
+constexpr int kOnePlaces = 64 * kSelectThreads;
 
 static size_t list_bytes(int64_t n_seq, int64_t count) { return ((size_t)n_seq * count * sizeof(int32_t) + 255) / 256 * 256; }
 static size_t hist_bytes(int64_t n_seq) { return (size_t)n_seq * 3 * kLongBins * sizeof(unsigned int); }

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_serving import BF16, F32, _attention, _cache, _check_mass, _check_out, _gen, bk  # noqa: F401  (bk: a fixture)
+from test_gpu_serving import BF16, F32, _attention, _cache, _check_evict, _check_mass, _check_out, _gen, bk  # noqa: F401  (bk: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -133,3 +133,20 @@ def test_a_query_of_nan(bk, dtype, n_seq, count, g, nq):  # noqa: F811
     assert bool(got[2][1][live].isnan().all()) and bool((got[2][1][~live] == 0).all())
     got[2][1] = ref[2][1]
     assert torch.equal(got[2], ref[2])
+
+
+@pytest.mark.parametrize("dtype,d,n_seq,count,keep", [(BF16, 64, 2, 32768, 9000), (BF16, 128, 1, 32769, 5), (F32, 64, 2, 50001, 50001), (BF16, 64, 3, 65536, 65535),
+                                                      (F32, 128, 1, 65536, 16384), (BF16, 64, 2, 65537, 16384), (BF16, 128, 2, 131072, 32768)])
+@pytest.mark.parametrize("masses", ["spread", "ties", "equal"])
+def test_evict_from_long_sequences(bk, dtype, d, n_seq, count, keep, masses):  # noqa: F811
+    """Both sides of what one workgroup has registers for."""
+    gen = _gen(count + keep)
+    K, V, w = _cache(gen, n_seq, count, d, dtype, absent=0.05)
+    mass = torch.exp(2.0 * torch.randn(n_seq, count, generator=gen, device="cuda"))
+    if masses == "ties":
+        mass = torch.floor(5.0 * torch.rand(n_seq, count, generator=gen, device="cuda"))
+    elif masses == "equal":
+        mass = torch.full_like(mass, 0.25)
+    sink, recent = min(4, keep), min(100, keep - min(4, keep))
+    res = bk.evict(bk.make_params(d, 64, 1, dtype, log_c=0.0), K, V, w, mass, keep, n_sink=sink, n_recent=recent)
+    _check_evict(res, K, V, w, mass, None, count, keep, sink, recent)
