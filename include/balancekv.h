@@ -425,7 +425,9 @@ int bkv_stream_attend(const bkv_stream* s, const void* Q, int32_t g, int32_t nq,
  * dispatch's own begin and end; up to n launches; creating the events allocates; not for use under
  * stream capture).  bkv_profile_read waits for the
  * recorded launches, returns how many were written and clears the log.  kind: 0 halving kernel,
- * 2 attend pass, 3 attend merge (1 is not in use); units: tokens the launch consumed.
+ * 2 attend pass (bkv_attend_mass: its second pass over the keys too), 3 attend merge (and what adds up
+ * masses), 4 eviction, the search (with few rows to move the copy as well), 5 eviction, the copy
+ * (1 is not in use); units: tokens the launch consumed (3: queries merged, or tokens whose masses it adds up).
  * bkv_profile_enable(0) turns it off.  Not thread-safe; off by default.                             */
 int bkv_profile_enable(int32_t max_records);
 int bkv_profile_read(int32_t* kind, float* ms, int64_t* units, int32_t cap);

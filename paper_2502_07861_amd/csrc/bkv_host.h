@@ -144,7 +144,7 @@ hipError_t launch_fill_iota(int32_t* idx, int64_t n_seq, int64_t seq_stride, int
                             hipStream_t st);
 
 // Opt-in per-launch timing (diagnostics): start/stop events attached to the launches themselves.
-enum { kProfCompress = 0, kProfAttend = 2, kProfAttendMerge = 3 };     // record kinds (1 is not in use)
+enum { kProfCompress = 0, kProfAttend = 2, kProfAttendMerge = 3, kProfEvict = 4, kProfEvictCopy = 5 };     // record kinds (1 is not in use)
 int prof_enable(int n);
 int prof_read(int32_t* kind, float* ms, int64_t* units, int cap);
 // Reserves a timing record and hands out its two events (false: timing is off or the records are used up).  The

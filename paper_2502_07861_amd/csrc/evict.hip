@@ -379,40 +379,36 @@ size_t evict_workspace_bytes(int64_t n_seq, int64_t count) {
 }
 
 template <int SLOTS>
-static void launch_gather(const EvictArgs& a, hipStream_t st) {
+static hipError_t launch_gather(const EvictArgs& a, hipStream_t st) {
     const int per = kGatherThreads / SLOTS * kGatherSteps;
     const int gx = (a.keep + per - 1) / per;
-    hipLaunchKernelGGL(evict_gather_kernel<SLOTS>, dim3((uint32_t)(gx > 65535 ? 65535 : gx), (uint32_t)a.n_seq), dim3(kGatherThreads), 0, st, a);
+    return launch_timed(kProfEvictCopy, a.n_seq * a.keep, evict_gather_kernel<SLOTS>, dim3((uint32_t)(gx > 65535 ? 65535 : gx), (uint32_t)a.n_seq), dim3(kGatherThreads), 0, st, a);
 }
 
 static hipError_t launch_long(const EvictArgs& a, hipStream_t st) {
     const dim3 grid((uint32_t)((a.count + kLongPlaces - 1) / kLongPlaces), (uint32_t)a.n_seq), block(kSelectThreads);
+    const int64_t units = a.n_seq * a.count;
     hipError_t e = launch_fill_u32(a.hist, 0u, a.n_seq * 3 * kLongBins, st);
-    for (int pass = 0; pass < 3 && e == hipSuccess; ++pass) {
-        hipLaunchKernelGGL(evict_count_kernel, grid, block, 0, st, a, pass);
-        e = hipGetLastError();
-    }
-    for (int list = 0; list < 2 && e == hipSuccess; ++list) {
-        hipLaunchKernelGGL(evict_list_kernel, grid, block, 0, st, a, list);
-        e = hipGetLastError();
-    }
+    for (int pass = 0; pass < 3 && e == hipSuccess; ++pass) e = launch_timed(kProfEvict, units, evict_count_kernel, grid, block, 0, st, a, pass);
+    for (int list = 0; list < 2 && e == hipSuccess; ++list) e = launch_timed(kProfEvict, units, evict_list_kernel, grid, block, 0, st, a, list);
     return e;
+}
+
+template <int KPT, int SLOTS = 0>
+static hipError_t launch_select(const EvictArgs& a, hipStream_t st) {
+    return launch_timed(kProfEvict, a.n_seq * a.count, evict_select_kernel<KPT, SLOTS>, dim3((uint32_t)a.n_seq), dim3(kSelectThreads), 0, st, a);
 }
 
 template <int SLOTS>
 static hipError_t launch_whole(const EvictArgs& a, hipStream_t st) {
-    const dim3 grid((uint32_t)a.n_seq), block(kSelectThreads);
-    if (a.count <= 4 * kSelectThreads) hipLaunchKernelGGL((evict_select_kernel<4, SLOTS>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((evict_select_kernel<16, SLOTS>), grid, block, 0, st, a);
-    return hipGetLastError();
+    return a.count <= 4 * kSelectThreads ? launch_select<4, SLOTS>(a, st) : launch_select<16, SLOTS>(a, st);
 }
 
 hipError_t launch_evict(EvictArgs& a, void* workspace, hipStream_t st) {
     a.pick = (int32_t*)workspace;
     a.hist = (unsigned int*)((char*)workspace + list_bytes(a.n_seq, a.count));
     a.chunk = (int2*)((char*)a.hist + hist_bytes(a.n_seq));
-    const dim3 grid((uint32_t)a.n_seq), block(kSelectThreads);
-    hipError_t e = hipSuccess;
+    hipError_t e;
     // Few rows: the workgroup that chose them moves them, one launch.  One compute unit copies slower than the launch of many takes from
     // here on.  Both sides, us a call, 8 sequences / the same in a captured graph / 256 sequences: 50 KB kept 8.5 for 11.9 / 8.5 for 8.7 / 12.1 for 14.3,
     // 128 KB (of 4000 places) 9.6 for 12.6 / 9.6 for 9.7 / 19.2 for 22.3, 256 KB 12.0 for 12.7 / 12.1 for 9.7 / 31.6 for 34.2, 500 KB 16.8 for 13.0.
@@ -422,19 +418,15 @@ hipError_t launch_evict(EvictArgs& a, void* workspace, hipStream_t st) {
         return launch_whole<32>(a, st);
     }
     if (a.count > kOnePlaces) e = launch_long(a, st);
-    else {
-        if (a.count <= 4 * kSelectThreads) hipLaunchKernelGGL(evict_select_kernel<4>, grid, block, 0, st, a);
-        else if (a.count <= 8 * kSelectThreads) hipLaunchKernelGGL(evict_select_kernel<8>, grid, block, 0, st, a);
-        else if (a.count <= 16 * kSelectThreads) hipLaunchKernelGGL(evict_select_kernel<16>, grid, block, 0, st, a);
-        else if (a.count <= 32 * kSelectThreads) hipLaunchKernelGGL(evict_select_kernel<32>, grid, block, 0, st, a);
-        else hipLaunchKernelGGL(evict_select_kernel<64>, grid, block, 0, st, a);
-        e = hipGetLastError();
-    }
+    else if (a.count <= 4 * kSelectThreads) e = launch_select<4>(a, st);
+    else if (a.count <= 8 * kSelectThreads) e = launch_select<8>(a, st);
+    else if (a.count <= 16 * kSelectThreads) e = launch_select<16>(a, st);
+    else if (a.count <= 32 * kSelectThreads) e = launch_select<32>(a, st);
+    else e = launch_select<64>(a, st);
     if (e != hipSuccess) return e;
-    if (a.row_bytes == 128) launch_gather<8>(a, st);
-    else if (a.row_bytes == 256) launch_gather<16>(a, st);
-    else launch_gather<32>(a, st);
-    return hipGetLastError();
+    if (a.row_bytes == 128) return launch_gather<8>(a, st);
+    if (a.row_bytes == 256) return launch_gather<16>(a, st);
+    return launch_gather<32>(a, st);
 }
 
 }  // namespace bkv

@@ -150,3 +150,22 @@ def test_evict_from_long_sequences(bk, dtype, d, n_seq, count, keep, masses):  #
     sink, recent = min(4, keep), min(100, keep - min(4, keep))
     res = bk.evict(bk.make_params(d, 64, 1, dtype, log_c=0.0), K, V, w, mass, keep, n_sink=sink, n_recent=recent)
     _check_evict(res, K, V, w, mass, None, count, keep, sink, recent)
+
+
+def test_launches_of_evict_are_recorded(bk):  # noqa: F811
+    """Few rows: one launch.  Many: search and copy.  Long sequences: three counts, two passes for the list, and the copy."""
+    from paper_2502_07861_amd import binding
+    p = bk.make_params(64, 64, 1, BF16, log_c=0.0)
+    gen = _gen(2)
+    for n_seq, count, keep, want in ((3, 500, 100, [4]), (2, 9000, 4000, [4, 5]), (1, 70000, 3000, [4, 4, 4, 4, 4, 5])):
+        K, V, w = _cache(gen, n_seq, count, 64, BF16)
+        mass = torch.rand(n_seq, count, generator=gen, device="cuda")
+        binding.profile_enable(16)
+        try:
+            bk.evict(p, K, V, w, mass, keep)
+            records = binding.profile_read(16)
+        finally:
+            binding.profile_enable(0)
+        assert [k for k, _, _ in records] == want
+        assert all(ms > 0 for _, ms, _ in records)
+        assert [u for _, _, u in records] == [n_seq * (count if k == 4 else keep) for k in want]
