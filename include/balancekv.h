@@ -238,7 +238,8 @@ int bkv_attend_prefix(const bkv_params* p, const void* K_p, const void* V_p, con
  * too: their P is 0).
  * visible       query i (0 <= i < nq) of every head sees the first visible + i places (none where that is not above 0); from
  *               `count` on all see everything.  The last nq tokens of a cache against it: count - nq + 1; a prompt against
- *               itself: 1.  What places hold that no query sees does not matter; value rows of tokens that some queries see
+ *               itself: 1.  Places count, with a token or without: sequences of different lengths in one call have to end at the
+ *               same place, their empty ones in front.  What places hold that no query sees does not matter; value rows of tokens that some queries see
  *               must be finite, as those that do not see them add them with weight 0.
  *               A query that holds a NaN makes the masses of its sequence's tokens NaN (those it does not see may be, too).
  * mass_in       [n_seq, stride_tokens] fp32 or NULL (zeros); may be mass_out.  decay in [0, 1]; with 0 it is not read.
@@ -254,7 +255,9 @@ int bkv_attend_mass(const bkv_params* p, const void* K_c, const void* V_c, const
 /* ---- eviction by accumulated attention weight ----------------------------------------------------------
  * Of the first `count` places of every sequence the first n_sink and the last n_recent stay, and the heaviest of the others,
  * `keep` in all (ties go to the lowest place; -0 is 0, a NaN counts as -inf), in ascending order, with their own weights.
- * A place whose weight w is not above 0 holds no token and never stays, in the windows neither.
+ * A place whose weight w is not above 0 holds no token and never stays, in the windows neither.  The windows are places: one of
+ * recent tokens wants sequences that end at the same place (empty places in front), one of first tokens such that begin there.
+ * In any other layout a mass of +infinity makes a window of any tokens: they stay before all others but the windows'.
  * K_c, V_c      [n_seq, stride_tokens, d]; w, mass [n_seq, stride_tokens] fp32; idx_in [n_seq, stride_tokens] int32 or NULL.
  * K_out, V_out  [n_seq, keep, d]; w_out, mass_out [n_seq, keep] fp32 or NULL; idx_out [n_seq, keep] int32 or NULL: idx_in of
  *               every kept token, or its place.  count_out [n_seq] int32 or NULL: tokens kept; behind them rows, w and mass

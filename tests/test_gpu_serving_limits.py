@@ -135,6 +135,60 @@ def test_a_query_of_nan(bk, dtype, n_seq, count, g, nq):  # noqa: F811
     assert torch.equal(got[2], ref[2])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("g,nq", [(2, 1), (4, 12), (2, 64)])
+def test_sequences_of_different_lengths_that_end_together(bk, dtype, g, nq):  # noqa: F811
+    """Empty places in front: the last nq tokens of every sequence see what lies before them, and a recent window holds last tokens."""
+    gen, n_seq, count, d = _gen(nq), 6, 500, 128
+    K, V, w = _cache(gen, n_seq, count, d, dtype, absent=0.0)
+    length = [500, 437, 64, 65, 1, 0]
+    for s, n in enumerate(length):
+        w[s, :count - n], K[s, :count - n], V[s, :count - n] = 0.0, float("nan"), float("inf")
+    Q = torch.randn(n_seq, g, nq, d, generator=gen, device="cuda").to(dtype)
+    p = bk.make_params(d, 64, 1, dtype, log_c=0.0)
+    out, lse, mass = bk.attend_mass(p, K, V, w, Q, visible=count - nq + 1)
+    kept = bk.evict(p, K, V, w, mass, 70, n_recent=20)
+    for s, n in enumerate(length):
+        own = slice(count - n, count)
+        sees = (n - nq + 1 + torch.arange(nq, device="cuda")).repeat(g)
+        ref = _attention(Q[s].reshape(-1, d), K[s, own], V[s, own], w[s, own], sees)
+        _check_out(out[s], lse[s], ref, dtype, count, "sequence %d" % s)
+        assert bool((mass[s, :count - n] == 0).all())
+        if n:
+            _check_mass(mass[s, own], mass[s, own], 0.0, ref, n, g * nq, "sequence %d" % s)
+        stay = min(n, 70)
+        assert int(kept["count"][s]) == stay
+        idx = kept["idx"][s, :stay].tolist()
+        assert idx == sorted(idx) and set(range(count - min(n, 20), count)) <= set(idx) <= set(range(count - n, count))
+        others = mass[s, own][:max(n - 20, 0)].sort(descending=True).values[:max(stay - 20, 0)]
+        assert torch.equal(kept["mass"][s, :max(stay - 20, 0)].sort(descending=True).values, others)
+
+
+@pytest.mark.parametrize("count,keep", [(900, 100), (70000, 5000)])
+def test_windows_of_sequences_that_begin_together(bk, count, keep):  # noqa: F811
+    """Empty places behind: a mass of +inf keeps a token before all others, so every sequence has windows at its own ends."""
+    gen, n_seq, d = _gen(count), 4, 64
+    K, V, w = _cache(gen, n_seq, count, d, BF16, absent=0.0)
+    mass = torch.rand(n_seq, count, generator=gen, device="cuda")
+    length = [count, count // 2 + 1, 40, 0]
+    marked = mass.clone()
+    for s, n in enumerate(length):
+        w[s, n:] = 0.0
+        marked[s, :min(n, 4)] = math.inf
+        marked[s, max(n - 30, 0):n] = math.inf
+    kept = bk.evict(bk.make_params(d, 64, 1, BF16, log_c=0.0), K, V, w, marked, keep)
+    for s, n in enumerate(length):
+        stay = min(n, keep)
+        assert int(kept["count"][s]) == stay
+        idx = kept["idx"][s, :stay].tolist()
+        window = set(range(min(n, 4))) | set(range(max(n - 30, 0), n))
+        assert idx == sorted(idx) and window <= set(idx) <= set(range(n))
+        rest = sorted(set(idx) - window)
+        outside = sorted(set(range(n)) - window)
+        want = mass[s][outside].sort(descending=True).values[:len(rest)] if outside else mass[s, :0]
+        assert torch.equal(mass[s][rest].sort(descending=True).values if rest else mass[s, :0], want)
+
+
 @pytest.mark.parametrize("dtype,d,n_seq,count,keep", [(BF16, 64, 2, 32768, 9000), (BF16, 128, 1, 32769, 5), (F32, 64, 2, 50001, 50001), (BF16, 64, 3, 65536, 65535),
                                                       (F32, 128, 1, 65536, 16384), (BF16, 64, 2, 65537, 16384), (BF16, 128, 2, 131072, 32768)])
 @pytest.mark.parametrize("masses", ["spread", "ties", "equal"])
