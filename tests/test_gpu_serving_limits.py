@@ -135,6 +135,49 @@ def test_a_query_of_nan(bk, dtype, n_seq, count, g, nq):  # noqa: F811
     assert torch.equal(got[2], ref[2])
 
 
+WHOLE = [  # dtype, d, n_seq, count, g, nq: sequences whose logits one workgroup holds (11 sixteenths of the compute units or more), up to what LDS takes and past it
+    (BF16, 128, 176, 2001, 4, 1), (F32, 128, 180, 777, 16, 1), (F32, 64, 177, 1001, 1, 1), (BF16, 128, 176, 8768, 4, 1), (BF16, 128, 176, 9152, 4, 1),
+    (BF16, 128, 176, 9153, 4, 1), (F32, 128, 180, 1488, 16, 1), (F32, 128, 180, 1489, 16, 1), (BF16, 64, 200, 4480, 8, 1), (BF16, 128, 520, 4576, 4, 1),
+    (BF16, 128, 520, 4577, 4, 1), (F32, 64, 176, 20320, 1, 2),
+]
+
+
+def _whole(bk, dtype, d, n_seq, count, g, nq):  # noqa: F811
+    gen = _gen(count + n_seq)
+    K, V, w = _cache(gen, n_seq, count, d, dtype)
+    Q = (2.0 * torch.randn(n_seq, g, nq, d, generator=gen, device="cuda")).to(dtype)
+    return K, V, w, Q, torch.rand(n_seq, count, generator=gen, device="cuda"), bk.make_params(d, 64, 1, dtype, log_c=0.0)
+
+
+@pytest.mark.parametrize("dtype,d,n_seq,count,g,nq", WHOLE)
+def test_mass_of_whole_sequences(bk, dtype, d, n_seq, count, g, nq):  # noqa: F811
+    K, V, w, Q, before, p = _whole(bk, dtype, d, n_seq, count, g, nq)
+    out, lse, mass = bk.attend_mass(p, K, V, w, Q, before, decay=0.5)
+    for s in range(0, n_seq, n_seq // 8):
+        ref = _attention(Q[s].reshape(-1, d), K[s], V[s], w[s])
+        _check_out(out[s], lse[s], ref, dtype, count, "sequence %d" % s)
+        _check_mass(mass[s], before[s], 0.5, ref, count, g * nq, "sequence %d" % s)
+
+
+@pytest.mark.parametrize("count", [9152, 9153])
+def test_the_longest_whole_sequences_captured(bk, count):  # noqa: F811
+    K, V, w, Q, before, p = _whole(bk, BF16, 128, 176, count, 4, 1)
+    ws = torch.empty(bk.attend_mass_workspace_bytes(p, 176, count, 4, 1), device="cuda", dtype=torch.uint8)
+    step = lambda: bk.attend_mass(p, K, V, w, Q, before, decay=0.5, workspace=ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for turn in range(3):
+        want = [t.clone() for t in step()]
+        for t in held:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want)), turn
+        Q.mul_(0.9)
+        before.add_(0.125)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("g,nq", [(2, 1), (4, 12), (2, 64)])
 def test_sequences_of_different_lengths_that_end_together(bk, dtype, g, nq):  # noqa: F811
