@@ -7,9 +7,10 @@
 // multiplied.  A wavefront has 32 queries in registers; where the workgroup has fewer than 128, wavefronts share queries and
 // split the keys of a tile.  Softmax weights stay in the lane that the next product wants them in (tile_device.h).
 //
-// What bounds it (bf16, d = 128): memory with few queries to a row (256 prefixes x 8192 tokens x 64 queries, 4096 x 301 own tokens: 276 us,
-// 6.2 TB/s), the matrix cores at the clock that they hold under this load, about 1.8 GHz, with hundreds (8 x 16385 tokens x 1280 queries 104 us, 840
-// TFLOP/s; 8 x 4096 tokens x 4 x 4096 queries, causal, 165 us, 830), start, two trips to memory and a store with little to do (8 x 4096 x 16: 7.9 us).
+// What bounds it (bf16, d = 128): memory with few queries to a row (256 prefixes x 8192 tokens x 64 queries, 4096 sequences of 151 own tokens on
+// average in 301 places: 277 us, 5.3 TB/s of rows that are fetched); with hundreds the products (45 % of the cycles) and the vector unit (43 %), which a
+// wavefront keeps busy in turn, two of them to a SIMD (8 x 16385 tokens x 1280 queries 136 us, 940 TFLOP/s with both numbers of a weight; 8 x 4096
+// tokens x 4 x 4096 queries, causal, 224 us, 920); start, two trips to memory and a store with little to do (8 x 4096 x 16: 8.2 us).
 #include <type_traits>
 
 #include "bkv_device.h"
@@ -493,8 +494,9 @@ static int tile_qw(int64_t rows) { return rows > 64 ? 4 : rows > 32 ? 2 : 1; }
 static int64_t tile_units(int64_t n_streams, int64_t rows, int qw) { return n_streams * ((rows + 32 * qw - 1) / (32 * qw)); }
 
 // Splits of a job of this shape at most (any token count; with fewer queries to a workgroup there are more workgroups, and fewer splits).
-// Causal jobs in fp32 may be cut twice as fine, as about half of their workgroups have little or nothing to do (1235 x 4 queries on 1235
-// tokens, 3 sequences, d = 128: 97 -> 75 us; bf16, whose cuts cost more than their work, 3156 x 4 queries: 60 -> 68).
+// Causal jobs in fp32 may be cut twice as fine, as about half of their workgroups have little or nothing to do (d = 128, us a call: 13 x 1959 x 1959
+// 396 -> 295, 9 x 730 x 4 x 730 166 -> 134, 3 x 1235 x 4 x 1235 as long).  bf16, where a cut costs more of its work, mostly takes as long either way
+// (8 x 687 x 8 x 687 48, 2118 x 8 x 2118, d = 64, 52; 3156 x 4 x 3156 63.5 -> 58).
 static int64_t tile_target(int elem, bool causal) { return elem == 4 && causal ? 2 * kTileTarget : kTileTarget; }
 int tile_most_splits(int64_t n_streams, int64_t rows, int elem, bool causal) {
     const int64_t wgs = tile_units(n_streams, rows, tile_qw(rows));
@@ -505,11 +507,11 @@ static bool tile_by_xcd(int64_t units) { return units % 8 == 0 || units >= 48; }
 
 // Splits of a job with workgroups of 128 queries (bf16: of 64 too), at most `most`: the least of (rounds of workgroups, by the fullest XCD) x (tiles of a split and
 // what a workgroup takes to begin and to end) + what the merge reads, in times of a tile; two workgroups of a compute unit side by side
-// take 1.5 times (fp32 1.8, causal bf16, of different lengths, 1.3) what one does.  `seen`: tiles that a query sees on average.  Against as many
-// splits as give two workgroups a compute unit, at least eight tiles each (bf16), us a call: 8 sequences x 420 tokens x 8 x 420 queries bf16 42 -> 33,
-// 106 prefixes x 199 x 200 bf16 36 -> 31, 13 x 1959 x 1959 fp32 390 -> 297, 9 x 730 x 4 x 730 fp32 158 -> 136, 8 x 8704 x 256 49.6 -> 47.4; workgroups
-// of 64: 106 prefixes x 487 x 42 24.6 -> 19.3, 6 x 3004 x 96 20.8 -> 17.2 (fp32 8 x 200 x 1120 22.5 -> 28.5: as they were); a few lose up to 6 %
-// (94 prefixes x 1543 x 34 bf16 32.5 -> 34.6) and one of 190 more (4 x 2616 x 75 18.6 -> 21.3).
+// take 1.5 times (fp32 1.8, causal bf16, of different lengths, 1.3) what one does.  `seen`: tiles that a query sees on average.  The constants are
+// fitted to such times.  As many splits as give two workgroups a compute unit (bf16, 128 queries: of at least eight tiles) / this, us a call, d = 128:
+// fp32 13 x 1959 x 1959 324 / 293, bf16 8 x 8704 x 256 52.8 / 49.5, 106 prefixes x 487 tokens x 40 queries 22.2 / 18.2, 6 x 3004 x 96 23.2 / 21.5,
+// equal within 2 %: 8 x 420 x 8 x 420, 8 x 4096 x 4 x 4096, 8 prefixes x 16385 x 1280, 106 x 199 x 200, 94 x 1543 x 34, 4 x 2616 x 75.  (Workgroups of 64 in fp32 lose:
+// 8 x 200 x 1120 22.5 / 28.5.)
 static int best_splits(int64_t n_streams, int n_qt, int tiles, int most, bool b16, bool causal, int seen) {
     const float side = !b16 ? 0.9f : causal ? 0.65f : 0.75f, ends = b16 ? 4.f : 1.f, merge = b16 ? 0.011f : 0.0025f;
     float least = 0.f;
@@ -537,8 +539,9 @@ void tile_plan(TileJob& j, int row_bytes, int elem, bool causal, int64_t taken, 
     for (j.qw = tile_qw(j.rows);; j.qw /= 2) {
         const int64_t wgs = tile_units(j.n_streams, j.rows, j.qw);
         j.n_qt = (j.rows + 32 * j.qw - 1) / (32 * j.qw);
-        // (A few others that the chip has no place for beside these cost a second round: 512 + 32 workgroups, two a compute unit, 11.6 us,
-        // 256 + 32 of them with twice the keys 7.7.  Many others are the launch's work themselves.)
+        // (A few others that the chip has no place for beside these cost a second round, so they are taken off: 8 x 64 tiles beside 32 workgroups
+        // may then be cut into 60, which whole tiles make 32 of two.  512 + 32 workgroups, two a compute unit, 11.6 us, 256 + 32 8.2.  Many
+        // others are the launch's work themselves.)
         int64_t splits = (tile_target(elem, causal) - (taken <= kTileTarget / 8 ? taken : 0)) / wgs;
         splits = max((int64_t)1, min(splits, (int64_t)tiles));
         if ((j.qw == 4 || (j.qw == 2 && elem == 2)) && tiles > 1) splits = best_splits(j.n_streams, j.n_qt, tiles, (int)splits, elem == 2, causal, seen);
