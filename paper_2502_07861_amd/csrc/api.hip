@@ -413,9 +413,10 @@ int bkv_attend_kv_static(const bkv_params* p, const void* K_c, const void* V_c, 
 // n stretches of len bytes, step bytes apart, from `at` on (null: nothing).
 struct Span { const void* at; size_t n, len, step; };
 static Span dense(const void* at, size_t bytes) { return {at, 1, bytes, bytes}; }
-// The first `count` of `stride` elements of every sequence.
+// The first `count` of `stride` elements of every sequence (one sequence may name any stride).
 static Span cache_span(const void* at, int64_t n_seq, int64_t count, int64_t stride, size_t elem) {
-    return {at, (size_t)n_seq, (size_t)count * elem, (size_t)stride * elem};
+    const size_t len = (size_t)count * elem, step = (size_t)stride * elem;
+    return {at, (size_t)n_seq, len, n_seq > 1 && step > len ? step : len};
 }
 
 // Does one of s's stretches reach into [lo, hi)?

@@ -80,3 +80,13 @@ def test_every_place(bk, seed):  # noqa: F811
         # the whole of K, V lies elsewhere
         got = _mass(bk, p, n_seq=n, count=count, stride=stride, visible=count, w=AT[2] + 4096, mass_out=AT[2] + 4096 + 4 * off)
         assert got == (bk.BKV_EINVAL if meet else bk.BKV_EWORKSPACE), (n, count, stride, off)
+
+
+def test_one_sequence_may_name_any_stride(bk):  # noqa: F811
+    p = bk.make_params(64, 64, 1, bk.BKV_F32, log_c=0.0)
+    for stride in (100, 2**56, 2**62, 2**63 - 1):                          # bytes past 64 bits
+        assert _mass(bk, p, n_seq=1, stride=stride) == bk.BKV_EWORKSPACE
+        assert _mass(bk, p, n_seq=1, stride=stride, out=AT[0] + 99 * 256) == bk.BKV_EINVAL
+        assert _mass(bk, p, n_seq=1, stride=stride, lse=AT[0] + 100 * 256) == bk.BKV_EWORKSPACE
+        assert _mass(bk, p, n_seq=1, stride=stride, mass_out=AT[4] + 4) == bk.BKV_EINVAL
+        assert _evict(bk, p, n_seq=1, stride=stride, ws=None) == bk.BKV_EWORKSPACE
