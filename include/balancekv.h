@@ -239,8 +239,8 @@ int bkv_attend_prefix(const bkv_params* p, const void* K_p, const void* V_p, con
  * visible       query i (0 <= i < nq) of every head sees the first visible + i places (none where that is not above 0); from
  *               `count` on all see everything.  The last nq tokens of a cache against it: count - nq + 1; a prompt against
  *               itself: 1.  Places count, with a token or without: sequences of different lengths in one call have to end at the
- *               same place, their empty ones in front.  What places hold that no query sees does not matter; value rows of tokens that some queries see
- *               must be finite, as those that do not see them add them with weight 0.
+ *               same place, their empty ones in front.  What places hold that no query sees does not matter; value rows of
+ *               tokens that some queries see must be finite, as those that do not see them add them with weight 0.
  *               A query that holds a NaN makes the masses of its sequence's tokens NaN (those it does not see may be, too).
  * mass_in       [n_seq, stride_tokens] fp32 or NULL (zeros); may be mass_out.  decay in [0, 1]; with 0 it is not read.
  * mass_out      [n_seq, stride_tokens]: places from `count` on are left as they are.  count == 0: untouched.

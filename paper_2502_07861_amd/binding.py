@@ -368,7 +368,8 @@ def attend_mass_workspace_bytes(p, n_seq, count, g, nq) -> int:
 def attend_mass(p, K_c, V_c, w, Q, mass=None, *, count=None, visible=None, decay=1.0, mass_out=None, workspace=None, out=None, lse=True):
     """bkv_attend_mass: attend_kv, and the tokens' accumulated attention weight.  K_c, V_c [n_seq, stride, d]; w, mass
     [n_seq, stride] (mass None: zeros); Q [n_seq, g, nq, d]; query i sees the first visible + i places (None: all), so
-    sequences of different lengths have to end at the same place.  mass_out may be mass.  Returns (out, lse or None, mass_out); a new mass_out is 0 from `count` on."""
+    sequences of different lengths have to end at the same place.  mass_out may be mass.  Returns (out, lse or None,
+    mass_out); a new mass_out is 0 from `count` on."""
     dt, f32, d = _torch_dtype(p), torch.float32, p.d
     n_seq, stride, _ = K_c.shape
     _, g, nq, _ = Q.shape
@@ -403,7 +404,8 @@ def evict_workspace_bytes(p, n_seq, count) -> int:
 
 def evict(p, K_c, V_c, w, mass, keep, *, n_sink=0, n_recent=0, count=None, idx=None, workspace=None, out=None):
     """bkv_evict: the heaviest `keep` tokens of every sequence by mass [n_seq, stride], those in the first n_sink and the last
-    n_recent of `count` places among them (tokens of other places stay first with a mass of inf).  Returns dict(K, V, w, mass, idx [n_seq, keep], count [n_seq]), `out` if it is given."""
+    n_recent of `count` places among them (tokens of other places stay first with a mass of inf).  Returns
+    dict(K, V, w, mass, idx [n_seq, keep], count [n_seq]), `out` if it is given."""
     dt, f32, d = _torch_dtype(p), torch.float32, p.d
     n_seq, stride, _ = K_c.shape
     dev = _device_of(K_c, "K_c")
